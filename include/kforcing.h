@@ -49,6 +49,7 @@ extern "C" {
 #define KF_FP32 0 /* weights, activations and KV cache in fp32 */
 #define KF_BF16 1 /* weights, GEMM inputs and KV cache in bf16; fp32 accumulation,
                      fp32 residual stream, fp32 noise sinusoid */
+#define KF_FP16 2 /* operators of the training step only (below); no model has it */
 
 #define KF_FLAG_DEBUG_LOGITS 1u /* reserve room for, and record, the fp32 head logits of
                                    the most recent step (kf_debug_logits) */
@@ -332,6 +333,156 @@ int kf_kernel_time(kf_ctx *ctx, int kernel_class, double *total_ms, int *launche
 #define KF_MASK_DOUBLE 1
 int kf_training_attention(void *hip_stream, int mask, int B, int H, int N, int k, int d_head,
                           const void *Q, const void *K, const void *V, void *O, float scale);
+
+/* kf_training_attention that also keeps, for the backward pass, each query
+ * row's natural log of the sum of exp(scale * q.k) over its visible keys:
+ * lse fp32 [B][H][rows].  O is kf_training_attention's bit for bit.  scale > 0,
+ * and keys * k below 2^32. */
+int kf_training_attention_lse(void *hip_stream, int mask, int B, int H, int N, int k, int d_head,
+                              const void *Q, const void *K, const void *V, void *O, float *lse,
+                              float scale);
+
+/* Gradients of kf_training_attention: with P = exp(scale Q K^T - lse) on the
+ * visible pairs and D = rowsum(dO O),
+ *     dV = P^T dO,  dS = P (dO V^T - D),  dQ = scale dS K,  dK = scale dS^T Q.
+ * O and lse are the forward call's, dO the gradient of O; dQ, dK and dV are
+ * written whole and must not overlap the inputs or each other.  Layouts, types
+ * (bf16; lse fp32), alignment, limits and errors as in kf_training_attention;
+ * P and dS are rounded to bf16 for the matrix products, all sums are fp32 and
+ * of a fixed order (no atomics: a call's result is the same on every run).
+ * Inputs are finite: an infinity or NaN may spread to rows and keys of its head
+ * that do not see it.  scale > 0, and keys * k below 2^32.
+ * workspace: kf_training_attention_backward_bytes() bytes of device memory,
+ * 16-byte aligned, used during the call only; calls that overlap need one
+ * each.  The size is 0 for arguments that the call refuses and for an empty
+ * problem (which launches nothing and leaves every pointer unchecked). */
+size_t kf_training_attention_backward_bytes(int mask, int B, int H, int N, int k, int d_head);
+int kf_training_attention_backward(void *hip_stream, int mask, int B, int H, int N, int k,
+                                   int d_head, const void *Q, const void *K, const void *V,
+                                   const void *O, const float *lse, const void *dO, void *dQ,
+                                   void *dK, void *dV, float scale, void *workspace,
+                                   size_t workspace_bytes);
+
+/* ------------------------------------------- operators of the training step
+ * What a student trained against the targets above needs beside its matrix
+ * products.  The calls are stateless, as kf_training_attention is: device
+ * pointers owned by the caller, work enqueued on hip_stream (null: the default
+ * stream) of the calling thread's current device, nothing allocated, nothing
+ * copied from or to the host, no clearing by the runtime (a call can be
+ * captured into a HIP graph), KF_EINVAL before any launch for a bad argument,
+ * KF_EHIP when a launch fails.  Sums have a fixed order: no atomics.  Types:
+ * KF_FP32, KF_BF16 and KF_FP16, rounded to nearest even where a result is
+ * stored, statistics and sums in fp32 (the gradient norm in fp64).  Pointers
+ * are aligned to their element.  Rows are d (or vocab) consecutive elements,
+ * ld* elements apart (ld >= the row's length; what lies between is neither
+ * read nor written). */
+
+/* Norms of rows.  KF_NORM_LAYER: y = (x - mu) r g + b, r = 1 / sqrt(var + eps);
+ * KF_NORM_RMS: y = x r g, r = 1 / sqrt(mean(x^2) + eps), no shift.
+ *   x [rows][d] of x_dtype, y of y_dtype: equal types, or x fp32 (a residual
+ *   stream) and y any.  gain [d] and shift [d] (null: no shift) are fp32.
+ *   stats fp32 [rows][2]: each row's (mu, r) for the backward pass, or null.
+ *   y may be x where types and ld agree; otherwise they must not overlap.
+ * 1 <= d <= 2^28, 0 <= rows (0: nothing launched), eps >= 0 and finite. */
+#define KF_NORM_LAYER 0
+#define KF_NORM_RMS 1
+int kf_layer_norm(void *hip_stream, int norm, int x_dtype, int y_dtype, int64_t rows, int d,
+                  const void *x, int64_t ldx, const float *gain, const float *shift, float eps,
+                  void *y, int64_t ldy, float *stats);
+
+/* Gradients of kf_layer_norm: with xh = (x - mu) r and w = dy g,
+ *     dx = r (w - mean(w) - xh mean(w xh)) + dres   (KF_NORM_RMS: no mean(w))
+ *     dgain = sum over rows of dy xh,  dshift = sum over rows of dy
+ *   dy [rows][d] of y_dtype; x, gain and stats as in the forward call; dx of
+ *   x_dtype; dres (null: none) of x_dtype is the gradient that reaches x past
+ *   the norm (a residual connection's), and dx may be dres (with its ld); dx
+ *   must not overlap x or dy.  dgain and dshift fp32 [d] are written, not
+ *   added to; either may be null (dshift must be for KF_NORM_RMS), and with
+ *   both null no workspace is needed.  With rows 0 they become zeros.
+ * workspace: kf_layer_norm_backward_bytes(rows, d) bytes of device memory,
+ * 16-byte aligned, used during the call only; calls that overlap need one
+ * each (two captured graphs that may run at once likewise). */
+size_t kf_layer_norm_backward_bytes(int64_t rows, int d);
+int kf_layer_norm_backward(void *hip_stream, int norm, int x_dtype, int y_dtype, int64_t rows,
+                           int d, const void *x, int64_t ldx, const float *gain,
+                           const float *stats, const void *dy, int64_t lddy, const void *dres,
+                           int64_t lddres, void *dx, int64_t lddx, float *dgain, float *dshift,
+                           void *workspace, size_t workspace_bytes);
+
+/* Log probabilities of given tokens under softmax(logits), logits [rows][vocab]
+ * of dtype: for each row
+ *     lse = log sum exp(l),  logp = l[token] - lse,  entropy = -sum p log p,
+ * and its n_top most probable alternatives, largest first, equal logits by the
+ * lower id (-0 equals 0, NaN counts as largest): top_ids int32 [rows][n_top]
+ * and their log probabilities top_logp fp32 [rows][n_top].
+ *   tokens int32 [rows], or null: no row has a token.  A negative token is a
+ *   row without one (logp 0); a token >= vocab gives logp NaN.
+ *   logp, entropy, lse: fp32 [rows], each may be null.
+ *   1 <= vocab <= 2^28, 0 <= n_top <= min(vocab, KF_MAX_TOP).
+ * Logits of minus infinity have probability 0.  A row of nothing else has lse,
+ * logp and top_logp minus infinity and entropy 0.  NaN or plus infinity in a
+ * row makes its results NaN (ids stay those of the order above). */
+#define KF_MAX_TOP 64
+int kf_token_logprobs(void *hip_stream, int dtype, int64_t rows, int vocab, const void *logits,
+                      int64_t ld, const int32_t *tokens, int n_top, float *logp, float *entropy,
+                      float *lse, int32_t *top_ids, float *top_logp);
+
+/* Gradient of the logits from those of logp (u) and entropy (c):
+ *     d_logits[v] = u ([v = token] - p_v) - c p_v (log p_v + entropy)
+ * d_logp, d_entropy fp32 [rows], either null: zeros.  The call reads the logits
+ * once and forms the rows' statistics itself, so it needs no forward call
+ * before it: where u and c are known beforehand (a weighted mean over rows),
+ * this call alone is the loss with its gradient; logp, entropy and lse (each
+ * may be null) are kf_token_logprobs's.  A row without a token has u = 0;
+ * a token >= vocab gives a row of NaN; a row of minus infinities gives zeros.
+ *   d_logits [rows][vocab] of dtype, ldd apart; it may be logits (ldd = ld),
+ *   otherwise they must not overlap. */
+int kf_token_logprobs_backward(void *hip_stream, int dtype, int64_t rows, int vocab,
+                               const void *logits, int64_t ld, const int32_t *tokens,
+                               const float *d_logp, const float *d_entropy, float *logp,
+                               float *entropy, float *lse, void *d_logits, int64_t ldd);
+
+/* The norm of a model's whole gradient and its clipping, over any number of
+ * tensors.  Each holds n consecutive elements src of src_dtype; the scaled
+ * gradient goes to dst: of the same type, or fp32 (half-precision gradients
+ * into an fp32 optimiser's).  dst may be src (same type) or null in a plan
+ * that only kf_grad_norm uses; other overlaps are not allowed. */
+typedef struct kf_grad {
+  const void *src;
+  void *dst;
+  int64_t n;
+  int src_dtype, dst_dtype;
+} kf_grad;
+
+/* A plan of the tensors: a table in device memory of the caller, and where it
+ * is.  It holds the tensors' addresses and is of use while they stay. */
+typedef struct kf_grad_plan {
+  void *dev;      /* kf_grad_plan_bytes() bytes, 256-byte aligned */
+  int64_t chunks; /* entries of the table */
+  int has_dst;    /* every tensor has a dst */
+} kf_grad_plan;
+
+/* Device bytes of a plan for the n tensors grads (a host array); 0 if an entry
+ * is invalid (an unknown type, n < 0, a null or misaligned pointer to
+ * elements). */
+size_t kf_grad_plan_bytes(int n, const kf_grad *grads);
+
+/* Build the plan in dev (on the stream; no copy from the host).  n = 0 is a
+ * plan of no tensors, whose norm is 0. */
+int kf_grad_plan_init(void *hip_stream, int n, const kf_grad *grads, void *dev, size_t bytes,
+                      kf_grad_plan *plan);
+
+/* norm (device, one fp32) = the root of the sum of all squares.  The squares
+ * are summed in fp64.  Calls with one plan use its device memory and must be
+ * ordered one after another. */
+int kf_grad_norm(void *hip_stream, const kf_grad_plan *plan, float *norm);
+
+/* dst = src * (norm > max_norm ? max_norm / norm : 1) for every tensor, and the
+ * norm before clipping into norm (device; may be null).  max_norm >= 0
+ * (infinity: never clip).  A norm that is not finite (infinities or NaN among
+ * the gradients) scales nothing: the caller sees it in norm.  KF_EINVAL for a
+ * plan with a tensor without a dst. */
+int kf_grad_clip(void *hip_stream, const kf_grad_plan *plan, float max_norm, float *norm);
 
 /* ----------------------------------------------------- continuous batching
  * Serving of independent sequences that start and end at different steps

@@ -9,15 +9,16 @@ computation happens here.  If the shared library is missing the import of
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libkforcing.so")
 
 KF_OK, KF_EINVAL, KF_ESTATE, KF_ECTX, KF_ENOMEM, KF_EHIP = 0, -1, -2, -3, -4, -5
-KF_FP32, KF_BF16 = 0, 1
+KF_FP32, KF_BF16, KF_FP16 = 0, 1, 2
 KF_FLAG_DEBUG_LOGITS = 1
 KF_FLAG_TEMPERATURE = 2
 KF_FLAG_TEACHER = 4
@@ -26,6 +27,8 @@ KF_FLAG_RMS_ROPE = 16
 KF_FLAG_SERVING = 32
 KF_PAGE = 128  # positions per KV page
 KF_MASK_SINGLE, KF_MASK_DOUBLE = 0, 1
+KF_NORM_LAYER, KF_NORM_RMS = 0, 1
+KF_MAX_TOP = 64
 KF_KC_NAMES = ["embed", "noise", "norm", "qkv", "attn", "oproj", "mlp_up", "mlp_down", "head",
                "select"]
 KF_TIMING_ALL = (1 << len(KF_KC_NAMES)) - 1
@@ -40,6 +43,15 @@ class KfConfig(ctypes.Structure):
         ("dtype", ctypes.c_int), ("max_batch", ctypes.c_int), ("max_k", ctypes.c_int),
         ("max_prompt", ctypes.c_int), ("flags", ctypes.c_uint), ("kv_pages", ctypes.c_int),
     ]
+
+
+class KfGrad(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("src_dtype", ctypes.c_int), ("dst_dtype", ctypes.c_int)]
+
+
+class KfGradPlan(ctypes.Structure):
+    _fields_ = [("dev", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("has_dst", ctypes.c_int)]
 
 
 class KfError(RuntimeError):
@@ -62,6 +74,7 @@ def lib():
                           "`python -m paper_2606_10820_amd.build` (there is no CPU fallback)")
     L = ctypes.CDLL(_LIB_PATH)
     P, I, U64, SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_size_t
+    I64, F = ctypes.c_int64, ctypes.c_float
     CP = ctypes.POINTER(KfConfig)
     IP = ctypes.POINTER(ctypes.c_int)
     sigs = {
@@ -90,6 +103,19 @@ def lib():
         "kf_last_error": (ctypes.c_char_p, [P]),
         "kf_strerror": (ctypes.c_char_p, [I]),
         "kf_training_attention": (I, [P, I, I, I, I, I, I, P, P, P, P, ctypes.c_float]),
+        "kf_training_attention_lse": (I, [P, I, I, I, I, I, I, P, P, P, P, P, F]),
+        "kf_training_attention_backward_bytes": (SZ, [I, I, I, I, I, I]),
+        "kf_training_attention_backward": (I, [P, I, I, I, I, I, I] + [P] * 9 + [F, P, SZ]),
+        "kf_layer_norm": (I, [P, I, I, I, I64, I, P, I64, P, P, F, P, I64, P]),
+        "kf_layer_norm_backward_bytes": (SZ, [I64, I]),
+        "kf_layer_norm_backward": (I, [P, I, I, I, I64, I, P, I64, P, P, P, I64, P, I64, P, I64,
+                                       P, P, P, SZ]),
+        "kf_token_logprobs": (I, [P, I, I64, I, P, I64, P, I, P, P, P, P, P]),
+        "kf_token_logprobs_backward": (I, [P, I, I64, I, P, I64, P, P, P, P, P, P, P, I64]),
+        "kf_grad_plan_bytes": (SZ, [I, P]),
+        "kf_grad_plan_init": (I, [P, I, P, P, SZ, ctypes.POINTER(KfGradPlan)]),
+        "kf_grad_norm": (I, [P, ctypes.POINTER(KfGradPlan), P]),
+        "kf_grad_clip": (I, [P, ctypes.POINTER(KfGradPlan), F, P]),
         "kf_serve_admit": (I, [P, I, P, I, P, I, P, P]),
         "kf_serve_step": (I, [P, I, P, I, P, P]),
         "kf_serve_release": (I, [P, I, P]),
@@ -390,3 +416,283 @@ def training_attention(mask: int, q, k_, v, N: int, k: int, scale: Optional[floa
     if rc != KF_OK:
         raise KfError(rc, lib().kf_strerror(rc).decode())
     return out
+
+
+# ------------------------------------------------ operators of the training step
+# Each call runs on `stream` (default: torch's current stream of the tensors'
+# device) and allocates its results there.
+
+_NOTHING = contextlib.nullcontext()
+
+
+def _ok(rc: int):
+    if rc != KF_OK:
+        raise KfError(rc, lib().kf_strerror(rc).decode())
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _on(device, stream, used):
+    """(raw stream, context to allocate and launch in) for tensors on `device`; the
+    caching allocator learns which tensors another stream uses."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    cur = torch.cuda.current_stream(device)
+    if stream is not None and stream != cur:
+        if stream.device != device:
+            raise ValueError("the stream is another device's")
+        for t in used:
+            if t is not None:
+                t.record_stream(stream)
+        return stream.cuda_stream, torch.cuda.stream(stream)
+    if torch.cuda.current_device() == device.index:
+        return cur.cuda_stream, _NOTHING
+    return cur.cuda_stream, torch.cuda.device(device)
+
+
+def _type(t, what: str) -> int:
+    import torch
+    code = {torch.float32: KF_FP32, torch.bfloat16: KF_BF16, torch.float16: KF_FP16}.get(t)
+    if code is None:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16")
+    return code
+
+
+def _rows(t, what: str, shape=None):
+    """(rows, ld) of t [..., d] seen as rows of d consecutive elements."""
+    if t.dim() < 1:
+        raise ValueError(f"{what} must have at least one dimension")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}")
+    d = t.shape[-1]
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, d) if t.numel() else t.new_empty((0, d))
+        except RuntimeError:
+            raise ValueError(f"{what}'s rows must be evenly spaced") from None
+    if d > 1 and t.stride(1) != 1 and t.numel():
+        raise ValueError(f"{what}'s last dimension must be contiguous")
+    return t.shape[0], (t.stride(0) if t.shape[0] > 1 else d)
+
+
+def _check(t, what: str, device, dtype, n: int):
+    """t (or None) holds n consecutive elements of dtype on device."""
+    if t is not None and (t.device != device or t.dtype != dtype or t.numel() != n
+                          or not t.is_contiguous()):
+        raise ValueError(f"{what} must be {n} contiguous {dtype} elements on {device}")
+
+
+def _attention_args(mask, q, k_, v, N, k, *more):
+    import torch
+    B, H, rows, dh = q.shape
+    if (rows, k_.shape[2]) != training_attention_shapes(mask, N, k):
+        raise ValueError("q/k rows do not match the mask's layout")
+    if k_.shape != v.shape or k_.shape[:2] != (B, H) or k_.shape[3] != dh:
+        raise ValueError("k and v must be [B][H][keys][dh] like q")
+    for t in (q, k_, v, *more):
+        if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.device != q.device:
+            raise ValueError("tensors must be contiguous bf16 on one device")
+    for t in more:
+        if t.shape != q.shape:
+            raise ValueError("out and dout must have q's shape")
+    return B, H, rows, dh
+
+
+def training_attention_lse(mask: int, q, k_, v, N: int, k: int, scale: Optional[float] = None,
+                           stream=None):
+    """training_attention that also returns each query row's log of the sum of exponentials,
+    (out, lse [B][H][rows] fp32), for training_attention_backward."""
+    import torch
+    B, H, rows, dh = _attention_args(mask, q, k_, v, N, k)
+    s, ctx = _on(q.device, stream, (q, k_, v))
+    with ctx:
+        out = torch.empty_like(q)
+        lse = torch.empty((B, H, rows), dtype=torch.float32, device=q.device)
+        _ok(lib().kf_training_attention_lse(s, mask, B, H, N, k, dh, q.data_ptr(), k_.data_ptr(),
+                                            v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                            dh ** -0.5 if scale is None else scale))
+    return out, lse
+
+
+def training_attention_backward(mask: int, q, k_, v, out, lse, dout, N: int, k: int,
+                                scale: Optional[float] = None, stream=None):
+    """Gradients (dq, dk, dv) of training_attention from the gradient dout of its output, with
+    out and lse of training_attention_lse (kf_training_attention_backward)."""
+    import torch
+    B, H, rows, dh = _attention_args(mask, q, k_, v, N, k, out, dout)
+    _check(lse, "lse", q.device, torch.float32, B * H * rows)
+    s, ctx = _on(q.device, stream, (q, k_, v, out, lse, dout))
+    with ctx:
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k_), torch.empty_like(v)
+        n = lib().kf_training_attention_backward_bytes(mask, B, H, N, k, dh)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+        _ok(lib().kf_training_attention_backward(
+            s, mask, B, H, N, k, dh, q.data_ptr(), k_.data_ptr(), v.data_ptr(), out.data_ptr(),
+            lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+            dh ** -0.5 if scale is None else scale, ws.data_ptr(), n))
+    return dq, dk, dv
+
+
+def layer_norm(x, gain, shift=None, eps: float = 1e-5, rms: bool = False, out_dtype=None,
+               out=None, stream=None):
+    """LayerNorm (or with rms RMSNorm) of the rows of x [..., d] (kf_layer_norm).
+
+    gain, shift [d] fp32.  Returns (y, stats): y like x in out_dtype (default x's;
+    another only for fp32 x), stats [rows][2] fp32 for layer_norm_backward."""
+    import torch
+    rows, ldx = _rows(x, "x")
+    d, dev = x.shape[-1], x.device
+    _check(gain, "gain", dev, torch.float32, d)
+    _check(shift, "shift", dev, torch.float32, d)
+    s, ctx = _on(dev, stream, (x, gain, shift, out))
+    with ctx:
+        if out is None:
+            y, ldy = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=dev), d
+        else:
+            y, (_, ldy) = out, _rows(out, "out", x.shape)
+            if y.device != dev or (out_dtype or y.dtype) != y.dtype:
+                raise ValueError("out must be on x's device and of out_dtype")
+        stats = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+        _ok(lib().kf_layer_norm(s, KF_NORM_RMS if rms else KF_NORM_LAYER, _type(x.dtype, "x"),
+                                _type(y.dtype, "out"), rows, d, x.data_ptr(), ldx, _ptr(gain),
+                                _ptr(shift), eps, y.data_ptr(), ldy, stats.data_ptr()))
+    return y, stats
+
+
+def layer_norm_backward(dy, x, gain, stats, rms: bool = False, dres=None, stream=None):
+    """Gradients of layer_norm (kf_layer_norm_backward): (dx, dgain, dshift), dx like x,
+    with dres (the gradient along the residual path, like x) added when given; dgain and
+    dshift [d] fp32, dshift None with rms."""
+    import torch
+    rows, ldx = _rows(x, "x")
+    _, lddy = _rows(dy, "dy", x.shape)
+    d, dev = x.shape[-1], x.device
+    lddres = d
+    if dres is not None:
+        _, lddres = _rows(dres, "dres", x.shape)
+        if dres.dtype != x.dtype or dres.device != dev:
+            raise ValueError("dres must be of x's type and device")
+    if dy.device != dev:
+        raise ValueError("dy must be on x's device")
+    _check(gain, "gain", dev, torch.float32, d)
+    _check(stats, "stats", dev, torch.float32, 2 * rows)
+    s, ctx = _on(dev, stream, (dy, x, gain, stats, dres))
+    with ctx:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        dgain = torch.empty(d, dtype=torch.float32, device=dev)
+        dshift = None if rms else torch.empty(d, dtype=torch.float32, device=dev)
+        n = lib().kf_layer_norm_backward_bytes(rows, d)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        _ok(lib().kf_layer_norm_backward(
+            s, KF_NORM_RMS if rms else KF_NORM_LAYER, _type(x.dtype, "x"), _type(dy.dtype, "dy"),
+            rows, d, x.data_ptr(), ldx, _ptr(gain), stats.data_ptr(), dy.data_ptr(), lddy,
+            _ptr(dres), lddres, dx.data_ptr(), d, dgain.data_ptr(), _ptr(dshift), ws.data_ptr(), n))
+    return dx, dgain, dshift
+
+
+class TokenLogprobs(NamedTuple):
+    logp: "torch.Tensor"
+    entropy: "torch.Tensor"
+    lse: "torch.Tensor"
+    top_ids: "Optional[torch.Tensor]" = None
+    top_logp: "Optional[torch.Tensor]" = None
+
+
+def token_logprobs(logits, tokens=None, n_top: int = 0, stream=None) -> TokenLogprobs:
+    """Log probabilities of tokens [...] int32 under softmax(logits [..., vocab]), with the
+    rows' entropies, log-sums and n_top most probable ids (kf_token_logprobs)."""
+    import torch
+    rows, ld = _rows(logits, "logits")
+    lead, V, dev = logits.shape[:-1], logits.shape[-1], logits.device
+    _check(tokens, "tokens", dev, torch.int32, rows)
+    s, ctx = _on(dev, stream, (logits, tokens))
+    with ctx:
+        logp, entropy, lse = (torch.empty(lead, dtype=torch.float32, device=dev) for _ in range(3))
+        ids = top = None
+        if n_top > 0:
+            ids = torch.empty((*lead, n_top), dtype=torch.int32, device=dev)
+            top = torch.empty((*lead, n_top), dtype=torch.float32, device=dev)
+        _ok(lib().kf_token_logprobs(s, _type(logits.dtype, "logits"), rows, V, logits.data_ptr(),
+                                    ld, _ptr(tokens), n_top, logp.data_ptr(), entropy.data_ptr(),
+                                    lse.data_ptr(), _ptr(ids), _ptr(top)))
+    return TokenLogprobs(logp, entropy, lse, ids, top)
+
+
+def token_logprobs_backward(logits, tokens, d_logp=None, d_entropy=None, out=None, stream=None):
+    """Gradient of logits [..., vocab] from the gradients d_logp and d_entropy [...] fp32 of
+    token_logprobs (kf_token_logprobs_backward; no forward call is needed before).  Returns
+    (d_logits, TokenLogprobs); out may be logits itself."""
+    import torch
+    rows, ld = _rows(logits, "logits")
+    lead, V, dev = logits.shape[:-1], logits.shape[-1], logits.device
+    _check(tokens, "tokens", dev, torch.int32, rows)
+    _check(d_logp, "d_logp", dev, torch.float32, rows)
+    _check(d_entropy, "d_entropy", dev, torch.float32, rows)
+    s, ctx = _on(dev, stream, (logits, tokens, d_logp, d_entropy, out))
+    with ctx:
+        logp, entropy, lse = (torch.empty(lead, dtype=torch.float32, device=dev) for _ in range(3))
+        if out is None:
+            out, ldd = torch.empty(logits.shape, dtype=logits.dtype, device=dev), V
+        else:
+            _, ldd = _rows(out, "out", logits.shape)
+            if out.dtype != logits.dtype or out.device != dev:
+                raise ValueError("out must be of logits' type and device")
+        _ok(lib().kf_token_logprobs_backward(
+            s, _type(logits.dtype, "logits"), rows, V, logits.data_ptr(), ld, _ptr(tokens),
+            _ptr(d_logp), _ptr(d_entropy), logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+            out.data_ptr(), ldd))
+    return out, TokenLogprobs(logp, entropy, lse)
+
+
+class GradClip:
+    """The norm of a list of gradients as a whole, and their clipping (kf_grad_norm,
+    kf_grad_clip): a plan over the tensors `grads`, which it keeps.
+
+    out: where the scaled gradients go, a tensor for each (of its type or fp32); default the
+    gradients themselves.  The plan is built on `stream` and used on one stream at a time."""
+
+    def __init__(self, grads, out=None, stream=None):
+        import torch
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        if len(self.out) != len(self.grads) or not self.grads:
+            raise ValueError("a plan takes one or more gradients and an out for each")
+        self.device = self.grads[0].device
+        arr = (KfGrad * len(self.grads))()
+        for i, (a, b) in enumerate(zip(self.grads, self.out)):
+            if a.device != self.device or b.device != self.device or a.numel() != b.numel():
+                raise ValueError("gradients and outs must match in size, on one device")
+            if not a.is_contiguous() or not b.is_contiguous():
+                raise ValueError("gradients and outs must be contiguous")
+            arr[i] = KfGrad(a.data_ptr(), b.data_ptr(), a.numel(), _type(a.dtype, "a gradient"),
+                            _type(b.dtype, "an out"))
+        n = lib().kf_grad_plan_bytes(len(self.grads), arr)
+        if n == 0:
+            raise KfError(KF_EINVAL, "kf_grad_plan_bytes rejected the tensors")
+        self.plan = KfGradPlan()
+        s, ctx = _on(self.device, stream, ())
+        with ctx:
+            self.buf = torch.empty(n + 256, dtype=torch.uint8, device=self.device)
+            _ok(lib().kf_grad_plan_init(s, len(self.grads), arr,
+                                        (self.buf.data_ptr() + 255) // 256 * 256, n,
+                                        ctypes.byref(self.plan)))
+
+    def _call(self, stream, f):
+        import torch
+        other = stream is not None and stream != torch.cuda.current_stream(self.device)
+        s, ctx = _on(self.device, stream, (self.buf, *self.grads, *self.out) if other else ())
+        with ctx:
+            norm = torch.empty((), dtype=torch.float32, device=self.device)
+            _ok(f(s, ctypes.byref(self.plan), norm.data_ptr()))
+        return norm
+
+    def norm(self, stream=None):
+        """The norm of all gradients, a 0-dimensional fp32 tensor."""
+        return self._call(stream, lib().kf_grad_norm)
+
+    def clip(self, max_norm: float, stream=None):
+        """Scale the gradients to at most max_norm into `out`; returns the norm before."""
+        return self._call(stream, lambda s, p, n: lib().kf_grad_clip(s, p, max_norm, n))

@@ -15,8 +15,10 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libkforcing.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 
-SOURCES = ["kf_api.cpp", "kf_kernels.hip", "kf_gemm.hip", "kf_blockattn.hip"]
-HEADERS = ["kf_internal.h", "kf_lds.h", "kf_attn.h", "kf_route.h"]
+SOURCES = ["kf_api.cpp", "kf_train_api.cpp", "kf_kernels.hip", "kf_gemm.hip", "kf_blockattn.hip",
+           "kf_attnbwd.hip", "kf_norm.hip", "kf_logprobs.hip", "kf_clip.hip"]
+HEADERS = ["kf_internal.h", "kf_lds.h", "kf_attn.h", "kf_route.h", "kf_blockattn.h", "kf_rows.h",
+           "kf_train.h"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -32,7 +34,8 @@ FLAGS = [
 # Per-source flags.  The training attention rescales its MFMA accumulators
 # with VALU code inside the key loop; its inline-asm LDS reads would otherwise
 # make the compiler keep the accumulators in AGPRs and copy them every tile.
-SOURCE_FLAGS = {"kf_blockattn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+SOURCE_FLAGS = {"kf_blockattn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+                "kf_attnbwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:

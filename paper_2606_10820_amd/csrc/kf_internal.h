@@ -409,7 +409,7 @@ int training_attention_rows(int mask, int N, int k);
 int training_attention_keys(int mask, int N, int k);
 hipError_t launch_training_attention(int mask, int B, int H, int N, int k, int dh, const bf16* Q,
                                      const bf16* K, const bf16* V, bf16* O, float scale,
-                                     hipStream_t s);
+                                     float* lse, hipStream_t s);  // lse: null, or the rows' log sums
 // The same with K, V holding ldk keys per head and O written as the rows of a
 // residual stream, [B][rows][H][dh].
 hipError_t launch_training_attention_seq(int mask, int B, int H, int N, int k, int dh, const bf16* Q,
