@@ -19,38 +19,69 @@ struct VecOf<T, 1> {
   typedef T type;
 };
 
+// In pieces of at most 16 bytes, which is all the alignment they need.
 template <int E, typename T>
 __device__ __forceinline__ void load_f(const T* __restrict__ p, float (&v)[E]) {
-  const typename VecOf<T, E>::type x = *reinterpret_cast<const typename VecOf<T, E>::type*>(p);
-  if constexpr (E == 1) {
-    v[0] = (float)x;
-  } else {
+  constexpr int P = E * sizeof(T) > 16 ? 16 / sizeof(T) : E;
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = (float)x[i];
+  for (int k = 0; k < E; k += P) {
+    const auto x = *reinterpret_cast<const typename VecOf<T, P>::type*>(p + k);
+    if constexpr (P == 1) {
+      v[k] = (float)x;
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[k + i] = (float)x[i];
+    }
   }
 }
 // One rounding to nearest even per element.
 template <int E, typename T>
 __device__ __forceinline__ void store_f(T* __restrict__ p, const float (&v)[E]) {
-  typename VecOf<T, E>::type x;
-  if constexpr (E == 1) {
-    x = (T)v[0];
-  } else {
+  constexpr int P = E * sizeof(T) > 16 ? 16 / sizeof(T) : E;
 #pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = (T)v[i];
+  for (int k = 0; k < E; k += P) {
+    typename VecOf<T, P>::type x;
+    if constexpr (P == 1) {
+      x = (T)v[k];
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) x[i] = (T)v[k + i];
+    }
+    *reinterpret_cast<typename VecOf<T, P>::type*>(p + k) = x;
   }
-  *reinterpret_cast<typename VecOf<T, E>::type*>(p) = x;
 }
 
-template <typename S>
-__device__ __forceinline__ S wave_add(S v) {
+// Reductions over a wavefront without LDS: rotations within 16 lanes, then two
+// lane swaps; every lane ends with the result, of the same order in every lane.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, F&& f) {
+  v = f(v, dpp<0x128>(v));  // row_ror:8, 4, 2, 1
+  v = f(v, dpp<0x124>(v));
+  v = f(v, dpp<0x122>(v));
+  v = f(v, dpp<0x121>(v));
+  const unsigned u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const unsigned w = __float_as_uint(v);
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float wave_add(float v) {
+  return wave_reduce(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {  // a NaN yields to a number
+  return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float wave_min(float v) {
+  return wave_reduce(v, [](float a, float b) { return fminf(a, b); });
+}
+__device__ __forceinline__ double wave_add(double v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
-}
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
   return v;
 }
 
