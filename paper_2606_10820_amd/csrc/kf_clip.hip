@@ -8,6 +8,8 @@
 // are and however long each is.  Sums of squares are fp64: no fp32 gradient
 // overflows or underflows them, and their order is fixed, so a norm is the same on
 // every run.
+#include <type_traits>
+
 #include "kf_rows.h"
 #include "kf_train.h"
 
@@ -40,14 +42,32 @@ __global__ void __launch_bounds__(256) grad_plan_kernel(PlanBatch b, GradChunk* 
   table[c] = o;
 }
 
+// Whole vectors of E elements, then the chunk's last elements one by one: f(index).
+template <int E, typename F, typename F1>
+__device__ __forceinline__ void over_chunk(int n, F&& f, F1&& f1) {
+  const int nv = n / E;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < nv; i += 256) f(i * E);
+  if (E > 1 && (int)threadIdx.x < n - nv * E) f1(nv * E + threadIdx.x);
+}
+
+__device__ __forceinline__ bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
 template <typename S>
 __device__ double chunk_sumsq(const GradChunk& c) {
   const S* x = static_cast<const S*>(c.src);
   double v = 0.0;
-  for (int i = threadIdx.x; i < c.n; i += 256) {
-    const double t = (double)(float)x[i];
-    v += t * t;
-  }
+  auto add = [&](auto e, int i) {
+    constexpr int E = decltype(e)::value;
+    float t[E];
+    load_f<E>(x + i, t);
+#pragma unroll
+    for (int j = 0; j < E; ++j) v = __builtin_fma((double)t[j], (double)t[j], v);
+  };
+  constexpr int VE = 16 / sizeof(S);
+  auto one = [&](int i) { add(std::integral_constant<int, 1>{}, i); };
+  if (on16(x)) over_chunk<VE>(c.n, [&](int i) { add(std::integral_constant<int, VE>{}, i); }, one);
+  else over_chunk<1>(c.n, one, one);
   return v;
 }
 
@@ -85,7 +105,18 @@ template <typename S, typename D>
 __device__ void chunk_scale(const GradChunk& c, float f) {
   const S* x = static_cast<const S*>(c.src);
   D* y = static_cast<D*>(c.dst);
-  for (int i = threadIdx.x; i < c.n; i += 256) y[i] = (D)((float)x[i] * f);
+  auto scale = [&](auto e, int i) {
+    constexpr int E = decltype(e)::value;
+    float t[E];
+    load_f<E>(x + i, t);
+#pragma unroll
+    for (int j = 0; j < E; ++j) t[j] *= f;
+    store_f<E>(y + i, t);
+  };
+  constexpr int VE = 16 / sizeof(S);
+  auto one = [&](int i) { scale(std::integral_constant<int, 1>{}, i); };
+  if (on16(x) && on16(y)) over_chunk<VE>(c.n, [&](int i) { scale(std::integral_constant<int, VE>{}, i); }, one);
+  else over_chunk<1>(c.n, one, one);
 }
 
 __global__ void __launch_bounds__(256)
@@ -96,7 +127,8 @@ __global__ void __launch_bounds__(256)
   if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = (float)v;
   // a norm that is not finite scales nothing
   const float f = v > (double)max_norm && v < (double)INFINITY ? (float)((double)max_norm / v) : 1.0f;
-  for (int64_t i = blockIdx.x; i < chunks; i += gridDim.x) {
+  // last chunks first: they are the ones that the caches still hold
+  for (int64_t i = chunks - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
     const GradChunk c = table[i];
     if (f == 1.0f && c.dst == c.src) continue;  // in place and unscaled: there already
     switch (c.types) {
