@@ -7,6 +7,7 @@
 // for the gradients u of logp and c of H.  Sums are fp32; a term whose e is zero
 // (a logit of minus infinity among them) adds nothing.  A row of nothing but
 // minus infinity has lse = logp = -inf, H = 0 and gradient 0.
+#include "kf_lds.h"
 #include "kf_rows.h"
 #include "kf_train.h"
 
@@ -24,26 +25,54 @@ __device__ __forceinline__ unsigned long long top_key(float x, int id) {
   return (unsigned long long)b << 32 | (unsigned)~id;
 }
 
-template <int NW>
-__device__ __forceinline__ unsigned long long block_max_key(unsigned long long v,
-                                                            unsigned long long* part) {
+// The largest key of a row's NT threads.
+template <int NT>
+__device__ __forceinline__ unsigned long long row_max_key(unsigned long long v, unsigned long long* part) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
     const unsigned long long o = __shfl_xor(v, off, 64);
     v = o > v ? o : v;
   }
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
+  if constexpr (NT > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = part[0];
 #pragma unroll
-  for (int i = 1; i < NW; ++i) v = part[i] > v ? part[i] : v;
-  __syncthreads();
+    for (int i = 1; i < NT / 64; ++i) v = part[i] > v ? part[i] : v;
+  }
   return v;
 }
 
+// The alternatives of any row: every thread keeps the best of its own elements
+// (tid, tid + NT, ...); each round takes the best of all, and its owner looks for its
+// next.  `part`: NT / 64 keys of LDS.
+template <typename T, int NT>
+__device__ __forceinline__ void top_rounds(const LogprobArgs& a, int64_t row, const T* x, int tid, float mr,
+                                        float ls, bool empty, unsigned long long* part) {
+  const int V = a.vocab;
+  unsigned long long best = 0;
+  for (int i = tid; i < V; i += NT) {
+    const unsigned long long k = top_key((float)x[i], i);
+    best = k > best ? k : best;
+  }
+  for (int j = 0; j < a.n_top; ++j) {
+    const unsigned long long k = row_max_key<NT>(best, part);
+    const int id = (int)~(unsigned)k;
+    if (id % NT == tid) {
+      a.top_ids[row * a.n_top + j] = id;
+      a.top_logp[row * a.n_top + j] = empty ? -INFINITY : ((float)x[id] - mr) - ls;
+      best = 0;
+      for (int i = tid; i < V; i += NT) {
+        const unsigned long long q = top_key((float)x[i], i);
+        if (q < k && q > best) best = q;
+      }
+    }
+  }
+}
+
 // A row of any length: a workgroup per row, one pass for the maximum, one for the
-// sums, one for the gradient.  Alternatives: every thread keeps the best of its own
-// elements; each round takes the best of all and its owner looks for its next.
+// sums, one for the gradient.
 template <typename T, int NW>
 __global__ void __launch_bounds__(64 * NW) logprobs_any_kernel(LogprobArgs a) {
   __shared__ float part[NW];
@@ -74,26 +103,7 @@ __global__ void __launch_bounds__(64 * NW) logprobs_any_kernel(LogprobArgs a) {
       if (a.entropy) a.entropy[row] = H;
       if (a.lse) a.lse[row] = lse;
     }
-    if (a.n_top) {
-      unsigned long long best = 0;
-      for (int i = tid; i < V; i += NT) {
-        const unsigned long long k = top_key((float)x[i], i);
-        best = k > best ? k : best;
-      }
-      for (int j = 0; j < a.n_top; ++j) {
-        const unsigned long long k = block_max_key<NW>(best, kpart);
-        const int id = (int)~(unsigned)k;
-        if (id % NT == tid) {  // this thread's element: store it, find the next
-          a.top_ids[row * a.n_top + j] = id;
-          a.top_logp[row * a.n_top + j] = empty ? -INFINITY : ((float)x[id] - mr) - ls;
-          best = 0;
-          for (int i = tid; i < V; i += NT) {
-            const unsigned long long q = top_key((float)x[i], i);
-            if (q < k && q > best) best = q;
-          }
-        }
-      }
-    }
+    if (a.n_top) top_rounds<T, NT>(a, row, x, tid, mr, ls, empty, kpart);
     if (a.d_logits) {
       T* dx = static_cast<T*>(a.d_logits) + row * a.ldd;
       float u = tok >= 0 && a.d_logp ? a.d_logp[row] : 0.f;
@@ -111,6 +121,268 @@ __global__ void __launch_bounds__(64 * NW) logprobs_any_kernel(LogprobArgs a) {
   }
 }
 
+// ---------------------------------------------------- rows held in registers
+// A row of up to NT * NV 16-byte vectors (and up to 2 (E - 1) elements around
+// them, where it starts or ends off a 16-byte boundary) is read once and kept, as
+// stored, in the registers of NT threads; every later use converts it again.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+  static constexpr int E = 4;
+  static constexpr unsigned kFill = 0xFF800000u;  // minus infinity
+  static __device__ __forceinline__ float get(const u32x4& v, int i) { return __uint_as_float(v[i]); }
+  static __device__ __forceinline__ u32x4 put(const float (&f)[4]) {
+    return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  }
+};
+template <>
+struct Raw<bf16> {
+  static constexpr int E = 8;
+  static constexpr unsigned kFill = 0xFF80FF80u;
+  static __device__ __forceinline__ float get(const u32x4& v, int i) {
+    return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
+  }
+  static __device__ __forceinline__ u32x4 put(const float (&f)[8]) {
+    typename VecOf<bf16, 8>::type o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = (bf16)f[i];
+    return __builtin_bit_cast(u32x4, o);
+  }
+};
+template <>
+struct Raw<f16> {
+  static constexpr int E = 8;
+  static constexpr unsigned kFill = 0xFC00FC00u;
+  static __device__ __forceinline__ float get(const u32x4& v, int i) {
+    return (float)__builtin_bit_cast(VecOf<f16, 8>::type, v)[i];
+  }
+  static __device__ __forceinline__ u32x4 put(const float (&f)[8]) {
+    VecOf<f16, 8>::type o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = (f16)f[i];
+    return __builtin_bit_cast(u32x4, o);
+  }
+};
+
+constexpr int kTopCap = 256;  // alternatives' candidates kept in LDS
+
+// One row's LDS.
+template <int NT>
+struct RowShared {
+  float m[NT / 64], s[NT / 64], w[NT / 64];
+  float lane_max[NT == 64 ? 1 : NT];
+  float t;
+  int count;
+  unsigned long long key[kTopCap];
+};
+
+// Orders this row's LDS writes before the reads that follow: a barrier, or, for a
+// row of one wavefront, program order.
+template <int NT>
+__device__ __forceinline__ void row_sync() {
+  if constexpr (NT > 64)
+    __syncthreads();
+  else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Wavefronts per SIMD that the registers are limited to: two workgroups of 1024 where
+// the row takes up to 32 registers, so that one loads while the other computes.
+constexpr int row_waves(int nt, int nv) { return nt == 1024 ? (nv <= 8 ? 8 : 4) : (nv <= 4 ? 8 : 6); }
+
+template <typename T, int NT, int NV, bool GRAD>
+__global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_waves_per_eu(row_waves(NT, NV))))
+    logprobs_row_kernel(LogprobArgs a) {
+  using R = Raw<T>;
+  constexpr int E = R::E, RPB = NT < 256 ? 256 / NT : 1, NW = NT / 64;
+  __shared__ RowShared<NT> shared[RPB];
+  RowShared<NT>& sh = shared[threadIdx.x / NT];
+  const int tid = threadIdx.x % NT, lane = tid & 63, V = a.vocab;
+  const int wv = __builtin_amdgcn_readfirstlane(tid & ~63);  // the wavefront's first thread
+  for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; row < a.rows; row += (int64_t)gridDim.x * RPB) {
+    const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+    const int head = min(V, (int)((-reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T)));
+    const int nb = (V - head) / E, tail0 = head + nb * E;  // vectors; first element past them
+    // this thread's element around the vectors, or none
+    const int edge = tid < head ? tid : (tid - head < V - tail0 ? tail0 + tid - head : -1);
+    const u32x4* xv = reinterpret_cast<const u32x4*>(x + head);
+    u32x4 r[NV];
+    float ex = -INFINITY;
+    if (edge >= 0) ex = (float)x[edge];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      r[j] = u32x4{R::kFill, R::kFill, R::kFill, R::kFill};
+      if (j * NT + tid < nb) r[j] = __builtin_nontemporal_load(xv + j * NT + tid);
+    }
+    const int tok = a.tokens ? a.tokens[row] : -1;
+    const float xt = tok >= 0 ? (tok < V ? (float)x[tok] : NAN) : 0.f;
+
+    // this thread's maximum, the wavefront's, and its sums against it
+    float tm = ex;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * NT + wv < nb) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) tm = fmaxf(tm, R::get(r[j], i));
+      }
+    // (pin: keep the row as it was read, not its converted elements)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) pin(r[j]);
+    float m = wave_max(tm);
+    float mr = m == -INFINITY ? 0.f : m;
+    float s, w;
+    {
+      const float t = (ex - mr) * kLog2e;
+      s = __builtin_amdgcn_exp2f(t);
+      w = s * fmaxf(t, -3e38f);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * NT + wv < nb) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float t = (R::get(r[j], i) - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
+          s += e;
+          w = __builtin_fmaf(e, fmaxf(t, -3e38f), w);
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) pin(r[j]);
+    s = wave_add(s);
+    w = wave_add(w);
+    if constexpr (NW > 1) {
+      // wavefronts' (m, s, w) joined: every wavefront forms the same sums
+      if (lane == 0) {
+        sh.m[tid >> 6] = m;
+        sh.s[tid >> 6] = s;
+        sh.w[tid >> 6] = w;
+      }
+      if (!GRAD && a.n_top) {
+        sh.lane_max[tid] = tm;
+        if (tid == 0) sh.count = 0;
+      }
+      __syncthreads();
+      const bool on = lane < NW;
+      const float mw = on ? sh.m[lane % NW] : -INFINITY;
+      const float sw = on ? sh.s[lane % NW] : 0.f, ww = on ? sh.w[lane % NW] : 0.f;
+      m = wave_max(mw);
+      mr = m == -INFINITY ? 0.f : m;
+      const float t = (mw - mr) * kLog2e, f = __builtin_amdgcn_exp2f(t);
+      s = wave_add(sw * f);
+      w = wave_add(f == 0.f || sw == 0.f ? 0.f : f * (ww + sw * t));  // (f = 0: t may be infinite)
+    } else if (!GRAD && a.n_top && tid == 0) {
+      sh.count = 0;
+    }
+    const bool empty = s == 0.f;
+    const float ls = logf(s), H = empty ? 0.f : ls - kLn2 * w / s;
+    if (tid == 0) {
+      if (a.logp) a.logp[row] = tok < 0 ? 0.f : (empty && tok < V ? -INFINITY : (xt - mr) - ls);
+      if (a.entropy) a.entropy[row] = H;
+      if (a.lse) a.lse[row] = mr + ls;
+    }
+    if constexpr (GRAD) {
+      // dl = -u p - c p (log p + H), and u at the token
+      T* dx = static_cast<T*>(a.d_logits) + row * a.ldd;
+      float u = tok >= 0 && a.d_logp ? a.d_logp[row] : 0.f;
+      if (tok >= V) u = NAN;
+      const float c = a.d_entropy ? a.d_entropy[row] : 0.f;
+      const float inv = empty ? 0.f : 1.0f / s, at = empty ? 0.f : u;
+      const float k0 = empty ? 0.f : -(u + c * (H - ls)) * inv, k1 = -c * kLn2 * inv;
+      auto grad = [&](float v) {
+        const float t = (v - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
+        // c = 0 leaves k1 zero, which a term of minus infinity would turn into NaN
+        return e * __builtin_fmaf(k1, fmaxf(t, -3e38f), k0);
+      };
+      const bool same = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(x)) & 15) == 0;
+      const int tv = tok >= head && tok < tail0 ? (tok - head) / E : -1;  // the token's vector
+      if (edge >= 0) dx[edge] = (T)(edge == tok ? at + grad(ex) : grad(ex));
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (j * NT + tid < nb) {
+          float d[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) d[i] = grad(R::get(r[j], i));
+          if (j * NT + tid == tv) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) d[i] += (tok - head) % E == i ? at : 0.f;
+          }
+          T* to = dx + head + (int64_t)(j * NT + tid) * E;
+          if (same) {
+            __builtin_nontemporal_store(R::put(d), reinterpret_cast<u32x4*>(to));
+          } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) to[i] = (T)d[i];
+          }
+        }
+    } else if (a.n_top) {
+      // Alternatives.  The 64 lanes (of all wavefronts) hold 64 sets of elements; a
+      // bound that n_top of the sets' maxima reach is one that the n_top largest
+      // elements reach.  The elements that reach it, few beyond n_top, are ranked
+      // against each other.  A row with NaN or plus infinity (s is NaN) or with too many
+      // of them goes the long way.
+      const int n = a.n_top;
+      bool slow = s != s;
+      if (wv == 0) {
+        float v = tm;
+        if constexpr (NW > 1) {
+#pragma unroll
+          for (int k = 1; k < NW; ++k) v = fmaxf(v, sh.lane_max[64 * k + lane]);
+        }
+        auto reach = [&](float b) { return __popcll(__builtin_amdgcn_ballot_w64(v >= b)) >= n; };
+        float lo = fmaxf(wave_min(v), -3.4028235e38f), hi = m;
+        if (!reach(lo)) {
+          lo = -INFINITY;
+        } else {
+          for (int k = 0; k < 10; ++k) {
+            const float mid = 0.5f * lo + 0.5f * hi;
+            if (reach(mid)) lo = mid;
+            else hi = mid;
+          }
+        }
+        if (lane == 0) sh.t = lo;
+      }
+      row_sync<NT>();
+      const float bound = sh.t;
+      if (!slow && __builtin_amdgcn_ballot_w64(tm >= bound)) {
+        auto offer = [&](float v, int id) {
+          if (v >= bound) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < kTopCap) sh.key[at] = top_key(v, id);
+          }
+        };
+        if (edge >= 0) offer(ex, edge);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (j * NT + tid < nb) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) offer(R::get(r[j], i), head + (j * NT + tid) * E + i);
+          }
+      }
+      row_sync<NT>();
+      const int count = sh.count;
+      slow |= count > kTopCap;
+      if (!slow) {
+        for (int i = tid; i < count; i += NT) {
+          const unsigned long long key = sh.key[i];
+          int rank = 0;
+          for (int k = 0; k < count; ++k) rank += sh.key[k] > key;
+          if (rank < n) {
+            const int id = (int)~(unsigned)key;
+            a.top_ids[row * n + rank] = id;
+            a.top_logp[row * n + rank] = empty ? -INFINITY : ((float)x[id] - mr) - ls;
+          }
+        }
+      } else {
+        top_rounds<T, NT>(a, row, x, tid, mr, ls, empty, sh.key);
+      }
+    }
+    if constexpr (NW > 1) __syncthreads();  // the next row's LDS
+  }
+}
+
 template <typename F>
 hipError_t by_type(int dtype, F&& f) {
   switch (dtype) {
@@ -123,10 +395,37 @@ hipError_t by_type(int dtype, F&& f) {
 
 }  // namespace
 
+namespace {
+
+template <typename T, int NT, int NV>
+hipError_t launch_row(const LogprobArgs& a, hipStream_t s) {
+  constexpr int RPB = NT < 256 ? 256 / NT : 1;
+  const int64_t blocks = (a.rows + RPB - 1) / RPB;
+  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), block(NT < 256 ? 256 : NT);
+  if (a.d_logits)
+    launch((logprobs_row_kernel<T, NT, NV, true>), grid, block, 0, s, a);
+  else
+    launch((logprobs_row_kernel<T, NT, NV, false>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t launch_token_logprobs(const LogprobArgs& a, hipStream_t s) {
   return by_type(a.dtype, [&](auto t) {
+    using T = decltype(t);
+    // threads and vectors per thread by the row's 16-byte vectors
+    const int nv = a.vocab / Raw<T>::E;
+    if (nv <= 64) return launch_row<T, 64, 1>(a, s);
+    if (nv <= 128) return launch_row<T, 64, 2>(a, s);
+    if (nv <= 256) return launch_row<T, 64, 4>(a, s);
+    if (nv <= 512) return launch_row<T, 64, 8>(a, s);
+    if (nv <= 2048) return launch_row<T, 256, 8>(a, s);
+    if (nv <= 4096) return launch_row<T, 1024, 4>(a, s);
+    if (nv <= 8192) return launch_row<T, 1024, 8>(a, s);
+    if (nv <= 16384) return launch_row<T, 1024, 16>(a, s);
     const dim3 grid((unsigned)(a.rows < 8192 ? a.rows : 8192));
-    launch((logprobs_any_kernel<decltype(t), 4>), grid, dim3(256), 0, s, a);
+    launch((logprobs_any_kernel<T, 16>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
   });
 }
