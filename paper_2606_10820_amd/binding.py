@@ -434,30 +434,45 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
+_current_raw = _current_device = None  # torch's, looked up on the first call
+
+
 def _on(device, stream, used):
     """(raw stream, context to allocate and launch in) for tensors on `device`; the
     caching allocator learns which tensors another stream uses."""
-    import torch
+    global _current_raw, _current_device
     if device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
-    cur = torch.cuda.current_stream(device)
-    if stream is not None and stream != cur:
+    import torch
+    if _current_device is None:
+        _current_device = torch.cuda.current_device
+        # the stream's handle without a Stream object (2 us a call), where torch has it
+        _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda i: torch.cuda.current_stream(i).cuda_stream)
+    raw = _current_raw(device.index)
+    if stream is not None and stream.cuda_stream != raw:
         if stream.device != device:
             raise ValueError("the stream is another device's")
         for t in used:
             if t is not None:
                 t.record_stream(stream)
         return stream.cuda_stream, torch.cuda.stream(stream)
-    if torch.cuda.current_device() == device.index:
-        return cur.cuda_stream, _NOTHING
-    return cur.cuda_stream, torch.cuda.device(device)
+    if _current_device() == device.index:
+        return raw, _NOTHING
+    return raw, torch.cuda.device(device)
+
+
+_CODES = {"torch.float32": KF_FP32, "torch.bfloat16": KF_BF16, "torch.float16": KF_FP16}
+_type_codes = {}  # the same by torch.dtype
 
 
 def _type(t, what: str) -> int:
-    import torch
-    code = {torch.float32: KF_FP32, torch.bfloat16: KF_BF16, torch.float16: KF_FP16}.get(t)
+    code = _type_codes.get(t)
     if code is None:
-        raise ValueError(f"{what} must be float32, bfloat16 or float16")
+        code = _CODES.get(str(t))
+        if code is None:
+            raise ValueError(f"{what} must be float32, bfloat16 or float16")
+        _type_codes[t] = code
     return code
 
 
@@ -595,33 +610,37 @@ def layer_norm_backward(dy, x, gain, stats, rms: bool = False, dres=None, stream
 
 class TokenLogprobs(NamedTuple):
     logp: "torch.Tensor"
-    entropy: "torch.Tensor"
-    lse: "torch.Tensor"
+    entropy: "Optional[torch.Tensor]" = None
+    lse: "Optional[torch.Tensor]" = None
     top_ids: "Optional[torch.Tensor]" = None
     top_logp: "Optional[torch.Tensor]" = None
 
 
-def token_logprobs(logits, tokens=None, n_top: int = 0, stream=None) -> TokenLogprobs:
+def token_logprobs(logits, tokens=None, n_top: int = 0, entropy: bool = True, lse: bool = False,
+                   stream=None) -> TokenLogprobs:
     """Log probabilities of tokens [...] int32 under softmax(logits [..., vocab]), with the
-    rows' entropies, log-sums and n_top most probable ids (kf_token_logprobs)."""
+    rows' entropies, log-sums (lse) and n_top most probable ids (kf_token_logprobs)."""
     import torch
     rows, ld = _rows(logits, "logits")
     lead, V, dev = logits.shape[:-1], logits.shape[-1], logits.device
     _check(tokens, "tokens", dev, torch.int32, rows)
     s, ctx = _on(dev, stream, (logits, tokens))
     with ctx:
-        logp, entropy, lse = (torch.empty(lead, dtype=torch.float32, device=dev) for _ in range(3))
+        logp = torch.empty(lead, dtype=torch.float32, device=dev)
+        H = torch.empty_like(logp) if entropy else None
+        ls = torch.empty_like(logp) if lse else None
         ids = top = None
         if n_top > 0:
             ids = torch.empty((*lead, n_top), dtype=torch.int32, device=dev)
             top = torch.empty((*lead, n_top), dtype=torch.float32, device=dev)
         _ok(lib().kf_token_logprobs(s, _type(logits.dtype, "logits"), rows, V, logits.data_ptr(),
-                                    ld, _ptr(tokens), n_top, logp.data_ptr(), entropy.data_ptr(),
-                                    lse.data_ptr(), _ptr(ids), _ptr(top)))
-    return TokenLogprobs(logp, entropy, lse, ids, top)
+                                    ld, _ptr(tokens), n_top, logp.data_ptr(), _ptr(H), _ptr(ls),
+                                    _ptr(ids), _ptr(top)))
+    return TokenLogprobs(logp, H, ls, ids, top)
 
 
-def token_logprobs_backward(logits, tokens, d_logp=None, d_entropy=None, out=None, stream=None):
+def token_logprobs_backward(logits, tokens, d_logp=None, d_entropy=None, out=None,
+                            entropy: bool = False, lse: bool = False, stream=None):
     """Gradient of logits [..., vocab] from the gradients d_logp and d_entropy [...] fp32 of
     token_logprobs (kf_token_logprobs_backward; no forward call is needed before).  Returns
     (d_logits, TokenLogprobs); out may be logits itself."""
@@ -633,7 +652,9 @@ def token_logprobs_backward(logits, tokens, d_logp=None, d_entropy=None, out=Non
     _check(d_entropy, "d_entropy", dev, torch.float32, rows)
     s, ctx = _on(dev, stream, (logits, tokens, d_logp, d_entropy, out))
     with ctx:
-        logp, entropy, lse = (torch.empty(lead, dtype=torch.float32, device=dev) for _ in range(3))
+        logp = torch.empty(lead, dtype=torch.float32, device=dev)
+        H = torch.empty_like(logp) if entropy else None
+        ls = torch.empty_like(logp) if lse else None
         if out is None:
             out, ldd = torch.empty(logits.shape, dtype=logits.dtype, device=dev), V
         else:
@@ -642,9 +663,8 @@ def token_logprobs_backward(logits, tokens, d_logp=None, d_entropy=None, out=Non
                 raise ValueError("out must be of logits' type and device")
         _ok(lib().kf_token_logprobs_backward(
             s, _type(logits.dtype, "logits"), rows, V, logits.data_ptr(), ld, _ptr(tokens),
-            _ptr(d_logp), _ptr(d_entropy), logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
-            out.data_ptr(), ldd))
-    return out, TokenLogprobs(logp, entropy, lse)
+            _ptr(d_logp), _ptr(d_entropy), logp.data_ptr(), _ptr(H), _ptr(ls), out.data_ptr(), ldd))
+    return out, TokenLogprobs(logp, H, ls)
 
 
 class GradClip:
@@ -680,13 +700,12 @@ class GradClip:
                                         (self.buf.data_ptr() + 255) // 256 * 256, n,
                                         ctypes.byref(self.plan)))
 
-    def _call(self, stream, f):
+    def _call(self, stream, f, *more):
         import torch
-        other = stream is not None and stream != torch.cuda.current_stream(self.device)
-        s, ctx = _on(self.device, stream, (self.buf, *self.grads, *self.out) if other else ())
+        s, ctx = _on(self.device, stream, (self.buf, *self.grads, *self.out) if stream else ())
         with ctx:
             norm = torch.empty((), dtype=torch.float32, device=self.device)
-            _ok(f(s, ctypes.byref(self.plan), norm.data_ptr()))
+            _ok(f(s, self.plan, *more, norm.data_ptr()))
         return norm
 
     def norm(self, stream=None):
@@ -695,4 +714,4 @@ class GradClip:
 
     def clip(self, max_norm: float, stream=None):
         """Scale the gradients to at most max_norm into `out`; returns the norm before."""
-        return self._call(stream, lambda s, p, n: lib().kf_grad_clip(s, p, max_norm, n))
+        return self._call(stream, lib().kf_grad_clip, max_norm)

@@ -101,6 +101,9 @@ __global__ void __launch_bounds__(256)
   if (threadIdx.x == 0) *norm = (float)v;
 }
 
+// Loads and stores that do not displace what the first pass left in the caches, in
+// vectors of the wider type (130 M gradients, bf16 into fp32: 234 -> 165 us; fp32 301 ->
+// 250).
 template <typename S, typename D>
 __device__ void chunk_scale(const GradChunk& c, float f) {
   const S* x = static_cast<const S*>(c.src);
@@ -108,12 +111,12 @@ __device__ void chunk_scale(const GradChunk& c, float f) {
   auto scale = [&](auto e, int i) {
     constexpr int E = decltype(e)::value;
     float t[E];
-    load_f<E>(x + i, t);
+    stream_in<E>(x + i, t);
 #pragma unroll
     for (int j = 0; j < E; ++j) t[j] *= f;
-    store_f<E>(y + i, t);
+    stream_out<E>(y + i, t);
   };
-  constexpr int VE = 16 / sizeof(S);
+  constexpr int VE = 16 / (sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D));
   auto one = [&](int i) { scale(std::integral_constant<int, 1>{}, i); };
   if (on16(x) && on16(y)) over_chunk<VE>(c.n, [&](int i) { scale(std::integral_constant<int, VE>{}, i); }, one);
   else over_chunk<1>(c.n, one, one);

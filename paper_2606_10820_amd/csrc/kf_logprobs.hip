@@ -25,6 +25,12 @@ __device__ __forceinline__ unsigned long long top_key(float x, int id) {
   return (unsigned long long)b << 32 | (unsigned)~id;
 }
 
+// The logit of a key (0 for -0; not for NaN).
+__device__ __forceinline__ float key_value(unsigned long long key) {
+  const unsigned b = (unsigned)(key >> 32);
+  return __uint_as_float(b & 0x80000000u ? b & 0x7FFFFFFFu : ~b);
+}
+
 // The largest key of a row's NT threads.
 template <int NT>
 __device__ __forceinline__ unsigned long long row_max_key(unsigned long long v, unsigned long long* part) {
@@ -71,60 +77,11 @@ __device__ __forceinline__ void top_rounds(const LogprobArgs& a, int64_t row, co
   }
 }
 
-// A row of any length: a workgroup per row, one pass for the maximum, one for the
-// sums, one for the gradient.
-template <typename T, int NW>
-__global__ void __launch_bounds__(64 * NW) logprobs_any_kernel(LogprobArgs a) {
-  __shared__ float part[NW];
-  __shared__ unsigned long long kpart[NW];
-  constexpr int NT = 64 * NW;
-  const int V = a.vocab, tid = threadIdx.x;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.logits) + row * a.ld;
-    float m = -INFINITY;
-    for (int i = tid; i < V; i += NT) m = fmaxf(m, (float)x[i]);
-    m = block_max<NW>(m, part);
-    const float mr = m == -INFINITY ? 0.f : m;
-    float s = 0.f, w = 0.f;
-    for (int i = tid; i < V; i += NT) {
-      const float t = ((float)x[i] - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
-      s += e;
-      w += e * fmaxf(t, -3e38f);
-    }
-    s = block_add<NW>(s, part);
-    w = block_add<NW>(w, part);
-    const float ls = logf(s), lse = mr + ls;
-    const bool empty = s == 0.f;
-    const float H = empty ? 0.f : ls - kLn2 * w / s;
-    const int tok = a.tokens ? a.tokens[row] : -1;
-    const float xt = tok >= 0 ? (tok < V ? (float)x[tok] : NAN) : 0.f;
-    if (tid == 0) {
-      if (a.logp) a.logp[row] = tok < 0 ? 0.f : (empty && tok < V ? -INFINITY : (xt - mr) - ls);
-      if (a.entropy) a.entropy[row] = H;
-      if (a.lse) a.lse[row] = lse;
-    }
-    if (a.n_top) top_rounds<T, NT>(a, row, x, tid, mr, ls, empty, kpart);
-    if (a.d_logits) {
-      T* dx = static_cast<T*>(a.d_logits) + row * a.ldd;
-      float u = tok >= 0 && a.d_logp ? a.d_logp[row] : 0.f;
-      if (tok >= V) u = NAN;
-      const float c = a.d_entropy ? a.d_entropy[row] : 0.f;
-      const float inv = empty ? 0.f : 1.0f / s;
-      for (int i = tid; i < V; i += NT) {
-        const float t = ((float)x[i] - mr) * kLog2e;
-        const float p = __builtin_amdgcn_exp2f(t) * inv;
-        float d = (i == tok && !empty ? u : 0.f) - u * p;
-        if (c != 0.f && p != 0.f) d -= c * p * ((t * kLn2 - ls) + H);
-        dx[i] = (T)d;
-      }
-    }
-  }
-}
-
-// ---------------------------------------------------- rows held in registers
-// A row of up to NT * NV 16-byte vectors (and up to 2 (E - 1) elements around
-// them, where it starts or ends off a 16-byte boundary) is read once and kept, as
-// stored, in the registers of NT threads; every later use converts it again.
+// A row is taken in 16-byte vectors from its first 16-byte boundary on, and up to
+// 2 (E - 1) elements around them.  Rows of up to NT * NV vectors are read once and kept,
+// as stored, in the registers of their NT threads; every later use converts them again.
+// Longer ones (NV = 0) are read once for the sums, with a running maximum, and once more
+// for the gradient or the alternatives.
 template <typename T>
 struct Raw;
 template <>
@@ -171,8 +128,7 @@ constexpr int kTopCap = 256;  // alternatives' candidates kept in LDS
 template <int NT>
 struct RowShared {
   float m[NT / 64], s[NT / 64], w[NT / 64];
-  float lane_max[NT == 64 ? 1 : NT];
-  float t;
+  float lane_max[NT];
   int count;
   unsigned long long key[kTopCap];
 };
@@ -181,100 +137,134 @@ struct RowShared {
 // row of one wavefront, program order.
 template <int NT>
 __device__ __forceinline__ void row_sync() {
-  if constexpr (NT > 64)
+  if constexpr (NT > 64) {
     __syncthreads();
-  else {
+  } else {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
 }
 
-// Wavefronts per SIMD that the registers are limited to: two workgroups of 1024 where
-// the row takes up to 32 registers, so that one loads while the other computes.
-constexpr int row_waves(int nt, int nv) { return nt == 1024 ? (nv <= 8 ? 8 : 4) : (nv <= 4 ? 8 : 6); }
+// Wavefronts per SIMD that the registers are limited to: two workgroups of 1024 (three
+// of 512) where the row takes up to 32 registers, so that some load while others compute.
+constexpr int row_waves(int nt, int nv) {
+  return nt == 1024 ? (nv > 8 ? 4 : 8) : (nv > 4 || nt * nv == 0 ? 6 : 8);
+}
 
 template <typename T, int NT, int NV, bool GRAD>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_waves_per_eu(row_waves(NT, NV))))
-    logprobs_row_kernel(LogprobArgs a) {
+    logprobs_kernel(LogprobArgs a) {
   using R = Raw<T>;
-  constexpr int E = R::E, RPB = NT < 256 ? 256 / NT : 1, NW = NT / 64;
+  constexpr int E = R::E, RPB = NT < 256 ? 256 / NT : 1, NW = NT / 64, NR = NV ? NV : 4;
   __shared__ RowShared<NT> shared[RPB];
   RowShared<NT>& sh = shared[threadIdx.x / NT];
   const int tid = threadIdx.x % NT, lane = tid & 63, V = a.vocab;
   const int wv = __builtin_amdgcn_readfirstlane(tid & ~63);  // the wavefront's first thread
-  for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; row < a.rows; row += (int64_t)gridDim.x * RPB) {
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; row < a.rows; row += step) {
     const T* x = static_cast<const T*>(a.logits) + row * a.ld;
     const int head = min(V, (int)((-reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T)));
     const int nb = (V - head) / E, tail0 = head + nb * E;  // vectors; first element past them
     // this thread's element around the vectors, or none
     const int edge = tid < head ? tid : (tid - head < V - tail0 ? tail0 + tid - head : -1);
     const u32x4* xv = reinterpret_cast<const u32x4*>(x + head);
-    u32x4 r[NV];
-    float ex = -INFINITY;
-    if (edge >= 0) ex = (float)x[edge];
+    const float ex = edge >= 0 ? (float)x[edge] : -INFINITY;
+    u32x4 r[NR];
+    auto load = [&](int first) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      r[j] = u32x4{R::kFill, R::kFill, R::kFill, R::kFill};
-      if (j * NT + tid < nb) r[j] = __builtin_nontemporal_load(xv + j * NT + tid);
-    }
+      for (int j = 0; j < NR; ++j) {
+        r[j] = u32x4{R::kFill, R::kFill, R::kFill, R::kFill};
+        if (first + j * NT + tid < nb) r[j] = __builtin_nontemporal_load(xv + first + j * NT + tid);
+      }
+    };
+    // f(vector, its index) over this thread's vectors; past the row's last one a
+    // wavefront's other lanes may still see vectors of minus infinity
+    auto each = [&](auto&& f, bool again = true) {
+#pragma unroll 1
+      for (int first = 0; first < (NV ? 1 : nb); first += NR * NT) {
+        if constexpr (NV == 0) load(first);
+        if (NV && again) {  // keep the row as it was read, not its converted elements
+#pragma unroll
+          for (int j = 0; j < NR; ++j) pin(r[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NR; ++j)
+          if (first + j * NT + wv < nb) f(r[j], first + j * NT + tid);
+      }
+    };
+    if constexpr (NV > 0) load(0);
     const int tok = a.tokens ? a.tokens[row] : -1;
     const float xt = tok >= 0 ? (tok < V ? (float)x[tok] : NAN) : 0.f;
 
-    // this thread's maximum, the wavefront's, and its sums against it
-    float tm = ex;
+    // this thread's maximum, and the wavefront's maximum and sums against it
+    float tm = ex, m, mr, s, w;
+    auto sum = [&](float v) {
+      const float t = (v - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
+      s += e;
+      w = __builtin_fmaf(e, fmaxf(t, -3e38f), w);
+    };
+    // (m, s, w) against the larger maximum `to`
+    auto rebase = [&](float from, float to) {
+      mr = to == -INFINITY ? 0.f : to;
+      const float t = (from - mr) * kLog2e, f = __builtin_amdgcn_exp2f(t);
+      w = f == 0.f || s == 0.f ? 0.f : f * (w + s * t);  // (f = 0: t may be infinite)
+      s *= f;
+    };
+    if constexpr (NV > 0) {
+      each([&](const u32x4& q, int) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j * NT + wv < nb) {
+        for (int i = 0; i < E; ++i) tm = fmaxf(tm, R::get(q, i));
+      }, false);
+      m = wave_max(tm);
+      mr = m == -INFINITY ? 0.f : m;
+      s = w = 0.f;
+      sum(ex);
+      each([&](const u32x4& q, int) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) tm = fmaxf(tm, R::get(r[j], i));
-      }
-    // (pin: keep the row as it was read, not its converted elements)
+        for (int i = 0; i < E; ++i) sum(R::get(q, i));
+      });
+    } else {
+      mr = ex == -INFINITY ? 0.f : ex;
+      s = w = 0.f;
+      sum(ex);
+      each([&](const u32x4& q, int) {
+        float c = R::get(q, 0);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) pin(r[j]);
-    float m = wave_max(tm);
-    float mr = m == -INFINITY ? 0.f : m;
-    float s, w;
-    {
-      const float t = (ex - mr) * kLog2e;
-      s = __builtin_amdgcn_exp2f(t);
-      w = s * fmaxf(t, -3e38f);
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j * NT + wv < nb) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const float t = (R::get(r[j], i) - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
-          s += e;
-          w = __builtin_fmaf(e, fmaxf(t, -3e38f), w);
+        for (int i = 1; i < E; ++i) c = fmaxf(c, R::get(q, i));
+        if (c > tm) {
+          rebase(tm, c);
+          tm = c;
         }
-      }
 #pragma unroll
-    for (int j = 0; j < NV; ++j) pin(r[j]);
+        for (int i = 0; i < E; ++i) sum(R::get(q, i));
+      });
+      m = wave_max(tm);
+      rebase(tm, m);
+    }
     s = wave_add(s);
     w = wave_add(w);
-    if constexpr (NW > 1) {
-      // wavefronts' (m, s, w) joined: every wavefront forms the same sums
+    const bool top = !GRAD && a.n_top > 0;
+    if constexpr (NW > 1) {  // the wavefronts' results joined, the same in every one
       if (lane == 0) {
         sh.m[tid >> 6] = m;
         sh.s[tid >> 6] = s;
         sh.w[tid >> 6] = w;
       }
-      if (!GRAD && a.n_top) {
-        sh.lane_max[tid] = tm;
-        if (tid == 0) sh.count = 0;
-      }
-      __syncthreads();
+      if (top) sh.lane_max[tid] = tm;
+    }
+    if (top && tid == 0) sh.count = 0;
+    // x[tok] has arrived before any thread goes on to write over it (d_logits = logits)
+    if (GRAD) asm volatile("" ::"v"(xt) : "memory");
+    row_sync<NT>();
+    if constexpr (NW > 1) {
       const bool on = lane < NW;
       const float mw = on ? sh.m[lane % NW] : -INFINITY;
-      const float sw = on ? sh.s[lane % NW] : 0.f, ww = on ? sh.w[lane % NW] : 0.f;
+      s = on ? sh.s[lane % NW] : 0.f;
+      w = on ? sh.w[lane % NW] : 0.f;
       m = wave_max(mw);
-      mr = m == -INFINITY ? 0.f : m;
-      const float t = (mw - mr) * kLog2e, f = __builtin_amdgcn_exp2f(t);
-      s = wave_add(sw * f);
-      w = wave_add(f == 0.f || sw == 0.f ? 0.f : f * (ww + sw * t));  // (f = 0: t may be infinite)
-    } else if (!GRAD && a.n_top && tid == 0) {
-      sh.count = 0;
+      rebase(mw, m);
+      s = wave_add(s);
+      w = wave_add(w);
     }
     const bool empty = s == 0.f;
     const float ls = logf(s), H = empty ? 0.f : ls - kLn2 * w / s;
@@ -299,87 +289,105 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
       const bool same = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(x)) & 15) == 0;
       const int tv = tok >= head && tok < tail0 ? (tok - head) / E : -1;  // the token's vector
       if (edge >= 0) dx[edge] = (T)(edge == tok ? at + grad(ex) : grad(ex));
+      each([&](const u32x4& q, int v) {
+        if (v >= nb) return;
+        float d[E];
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (j * NT + tid < nb) {
-          float d[E];
+        for (int i = 0; i < E; ++i) d[i] = grad(R::get(q, i));
+        if (v == tv) {
 #pragma unroll
-          for (int i = 0; i < E; ++i) d[i] = grad(R::get(r[j], i));
-          if (j * NT + tid == tv) {
-#pragma unroll
-            for (int i = 0; i < E; ++i) d[i] += (tok - head) % E == i ? at : 0.f;
-          }
-          T* to = dx + head + (int64_t)(j * NT + tid) * E;
-          if (same) {
-            __builtin_nontemporal_store(R::put(d), reinterpret_cast<u32x4*>(to));
-          } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) to[i] = (T)d[i];
-          }
+          for (int i = 0; i < E; ++i) d[i] += (tok - head) % E == i ? at : 0.f;
         }
-    } else if (a.n_top) {
+        T* to = dx + head + (int64_t)v * E;
+        if (same) {
+          __builtin_nontemporal_store(R::put(d), reinterpret_cast<u32x4*>(to));
+        } else {
+#pragma unroll
+          for (int i = 0; i < E; ++i) to[i] = (T)d[i];
+        }
+      });
+    } else if (top) {
       // Alternatives.  The 64 lanes (of all wavefronts) hold 64 sets of elements; a
       // bound that n_top of the sets' maxima reach is one that the n_top largest
       // elements reach.  The elements that reach it, few beyond n_top, are ranked
       // against each other.  A row with NaN or plus infinity (s is NaN) or with too many
-      // of them goes the long way.
+      // of them (equal logits) goes the long way.
       const int n = a.n_top;
-      bool slow = s != s;
-      if (wv == 0) {
-        float v = tm;
-        if constexpr (NW > 1) {
+      float v = tm;
+      if constexpr (NW > 1) {
 #pragma unroll
-          for (int k = 1; k < NW; ++k) v = fmaxf(v, sh.lane_max[64 * k + lane]);
-        }
-        auto reach = [&](float b) { return __popcll(__builtin_amdgcn_ballot_w64(v >= b)) >= n; };
-        float lo = fmaxf(wave_min(v), -3.4028235e38f), hi = m;
-        if (!reach(lo)) {
-          lo = -INFINITY;
-        } else {
-          for (int k = 0; k < 10; ++k) {
-            const float mid = 0.5f * lo + 0.5f * hi;
-            if (reach(mid)) lo = mid;
-            else hi = mid;
-          }
-        }
-        if (lane == 0) sh.t = lo;
+        for (int k = 0; k < NW; ++k) v = fmaxf(v, sh.lane_max[64 * k + lane]);
       }
-      row_sync<NT>();
-      const float bound = sh.t;
-      if (!slow && __builtin_amdgcn_ballot_w64(tm >= bound)) {
-        auto offer = [&](float v, int id) {
-          if (v >= bound) {
+      auto reach = [&](float b) { return __popcll(__builtin_amdgcn_ballot_w64(v >= b)) >= n; };
+      float bound = fmaxf(wave_min(v), -3.4028235e38f), hi = m;
+      if (!reach(bound)) {
+        bound = -INFINITY;
+      } else {
+#pragma unroll 1
+        for (int k = 0; k < 10; ++k) {
+          const float mid = 0.5f * bound + 0.5f * hi;
+          if (reach(mid)) bound = mid;
+          else hi = mid;
+        }
+      }
+      if (s == s && __builtin_amdgcn_ballot_w64(tm >= bound)) {
+        auto offer = [&](float f, int id) {
+          if (f >= bound) {
             const int at = atomicAdd(&sh.count, 1);
-            if (at < kTopCap) sh.key[at] = top_key(v, id);
+            if (at < kTopCap) sh.key[at] = top_key(f, id);
           }
         };
         if (edge >= 0) offer(ex, edge);
+        auto offer_all = [&](const u32x4& q, int k) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-          if (j * NT + tid < nb) {
+          for (int i = 0; i < E; ++i) offer(R::get(q, i), head + k * E + i);
+        };
+        if constexpr (NV > 0) {
+          each([&](const u32x4& q, int k) {
+            if (k < nb && tm >= bound) offer_all(q, k);
+          });
+        } else {
+          // read again, all lanes together: a thread's vectors whose maximum reaches it
+          unsigned long long who = __builtin_amdgcn_ballot_w64(tm >= bound);
+          while (who) {
+            int of[4];
 #pragma unroll
-            for (int i = 0; i < E; ++i) offer(R::get(r[j], i), head + (j * NT + tid) * E + i);
+            for (int j = 0; j < 4; ++j) {
+              of[j] = who ? wv + __builtin_ctzll(who) : nb;
+              who &= who - 1;
+            }
+            for (int i = lane * NT; i < nb; i += 64 * NT) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                r[j] = u32x4{R::kFill, R::kFill, R::kFill, R::kFill};
+                if (of[j] + i < nb) r[j] = xv[of[j] + i];
+              }
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (of[j] + i < nb) offer_all(r[j], of[j] + i);
+            }
           }
+        }
       }
       row_sync<NT>();
       const int count = sh.count;
-      slow |= count > kTopCap;
-      if (!slow) {
+      if (s == s && count <= kTopCap) {
         for (int i = tid; i < count; i += NT) {
           const unsigned long long key = sh.key[i];
           int rank = 0;
+#pragma unroll 4
           for (int k = 0; k < count; ++k) rank += sh.key[k] > key;
           if (rank < n) {
-            const int id = (int)~(unsigned)key;
-            a.top_ids[row * n + rank] = id;
-            a.top_logp[row * n + rank] = empty ? -INFINITY : ((float)x[id] - mr) - ls;
+            a.top_ids[row * n + rank] = (int)~(unsigned)key;
+            a.top_logp[row * n + rank] = empty ? -INFINITY : (key_value(key) - mr) - ls;
           }
         }
       } else {
+        row_sync<NT>();  // the keys make room
         top_rounds<T, NT>(a, row, x, tid, mr, ls, empty, sh.key);
       }
     }
-    if constexpr (NW > 1) __syncthreads();  // the next row's LDS
+    if (NW > 1 && row + step < a.rows) __syncthreads();  // the next row's LDS
   }
 }
 
@@ -397,16 +405,40 @@ hipError_t by_type(int dtype, F&& f) {
 
 namespace {
 
-template <typename T, int NT, int NV>
-hipError_t launch_row(const LogprobArgs& a, hipStream_t s) {
+template <typename T, int NT, int NV, bool GRAD>
+hipError_t launch_rows(const LogprobArgs& a, hipStream_t s) {
   constexpr int RPB = NT < 256 ? 256 / NT : 1;
   const int64_t blocks = (a.rows + RPB - 1) / RPB;
-  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), block(NT < 256 ? 256 : NT);
-  if (a.d_logits)
-    launch((logprobs_row_kernel<T, NT, NV, true>), grid, block, 0, s, a);
-  else
-    launch((logprobs_row_kernel<T, NT, NV, false>), grid, block, 0, s, a);
+  launch((logprobs_kernel<T, NT, NV, GRAD>), dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)),
+         dim3(NT < 256 ? 256 : NT), 0, s, a);
   return hipGetLastError();
+}
+
+// Threads, and vectors a thread holds, by a row's 16-byte vectors.  The gradient needs a
+// row twice, so a row stays in registers as long as they hold it; the sums alone stream
+// it from 2049 vectors on, which keeps more rows in flight.  us, plain | with 8
+// alternatives, held in registers and streamed in 256, 512, 1024 threads:
+//   8192 x 30522 bf16 103 | 116,  95 | 118, 108 | 124, 126 | 149
+//   4096 x 50257 bf16  83 | 101,  73 |  93,  75 |  92,  88 |  99
+//   2048 x 50257 fp32  85 | 109,  68 |  88,  76 |  86,  65 |  72
+//   4 x 50257 fp32 streamed 12.3 | 14.2, 9.0 | 12.2, 8.8 | 11.6
+template <typename T, bool GRAD>
+hipError_t launch_by_width(const LogprobArgs& a, hipStream_t s) {
+  const int nv = a.vocab / Raw<T>::E;
+  if (nv <= 64) return launch_rows<T, 64, 1, GRAD>(a, s);
+  if (nv <= 128) return launch_rows<T, 64, 2, GRAD>(a, s);
+  if (nv <= 256) return launch_rows<T, 64, 4, GRAD>(a, s);
+  if (nv <= 512) return launch_rows<T, 64, 8, GRAD>(a, s);
+  if (nv <= 2048) return launch_rows<T, 256, 8, GRAD>(a, s);
+  if constexpr (GRAD) {
+    if (nv <= 4096) return launch_rows<T, 512, 8, GRAD>(a, s);
+    if (nv <= 8192) return launch_rows<T, 1024, 8, GRAD>(a, s);
+    if (nv <= 16384) return launch_rows<T, 1024, 16, GRAD>(a, s);
+  } else if (a.rows > 256) {  // (fewer: the latency of a row counts, 1024 threads)
+    if (nv <= 4096) return launch_rows<T, 256, 0, GRAD>(a, s);
+    if (sizeof(T) == 2) return launch_rows<T, 512, 0, GRAD>(a, s);
+  }
+  return launch_rows<T, 1024, 0, GRAD>(a, s);
 }
 
 }  // namespace
@@ -414,19 +446,7 @@ hipError_t launch_row(const LogprobArgs& a, hipStream_t s) {
 hipError_t launch_token_logprobs(const LogprobArgs& a, hipStream_t s) {
   return by_type(a.dtype, [&](auto t) {
     using T = decltype(t);
-    // threads and vectors per thread by the row's 16-byte vectors
-    const int nv = a.vocab / Raw<T>::E;
-    if (nv <= 64) return launch_row<T, 64, 1>(a, s);
-    if (nv <= 128) return launch_row<T, 64, 2>(a, s);
-    if (nv <= 256) return launch_row<T, 64, 4>(a, s);
-    if (nv <= 512) return launch_row<T, 64, 8>(a, s);
-    if (nv <= 2048) return launch_row<T, 256, 8>(a, s);
-    if (nv <= 4096) return launch_row<T, 1024, 4>(a, s);
-    if (nv <= 8192) return launch_row<T, 1024, 8>(a, s);
-    if (nv <= 16384) return launch_row<T, 1024, 16>(a, s);
-    const dim3 grid((unsigned)(a.rows < 8192 ? a.rows : 8192));
-    launch((logprobs_any_kernel<T, 16>), grid, dim3(1024), 0, s, a);
-    return hipGetLastError();
+    return a.d_logits ? launch_by_width<T, true>(a, s) : launch_by_width<T, false>(a, s);
   });
 }
 

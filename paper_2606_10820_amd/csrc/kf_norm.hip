@@ -17,9 +17,13 @@
 namespace kf {
 namespace {
 
-// Rows held in registers: WPR wavefronts a row, EPL elements a lane in vectors of E.
-// Element j of this lane's vector v is column (v * 64 WPR + lane) * E + j.
-template <int E, int EPL, int WPR>
+// Rows held in registers: LPR lanes of a workgroup of 512 a row (16 and 32: rows
+// share a wavefront; more than 64: a row spans wavefronts), EPL elements a lane in
+// vectors of E.  Element j of lane l's vector v is column (v * LPR + l) * E + j.  Lanes
+// past the last column load the first one's elements, so that no load hangs on a
+// branch, and are zeroed where they would count.
+constexpr int kNormThreads = 512;
+template <int E, int EPL, int LPR>
 struct Cols {
   static constexpr int NV = EPL / E;
   int col[NV];
@@ -27,59 +31,74 @@ struct Cols {
   __device__ __forceinline__ Cols(int tid, int d) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      col[v] = (v * 64 * WPR + tid) * E;
-      on[v] = col[v] < d;
+      const int c = (v * LPR + tid) * E;
+      on[v] = c < d;
+      col[v] = on[v] ? c : 0;
     }
   }
   template <typename T>
   __device__ __forceinline__ void load(float (&f)[NV][E], const T* p) const {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
+    for (int v = 0; v < NV; ++v) load_f<E>(p + col[v], f[v]);
+  }
+  template <typename T>  // not read again soon
+  __device__ __forceinline__ void stream(float (&f)[NV][E], const T* p) const {
 #pragma unroll
-      for (int j = 0; j < E; ++j) f[v][j] = 0.f;
-      if (on[v]) load_f<E>(p + col[v], f[v]);
-    }
+    for (int v = 0; v < NV; ++v) stream_in<E>(p + col[v], f[v]);
+  }
+  __device__ __forceinline__ void zero(float (&f)[NV][E], bool live) const {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < E; ++j) f[v][j] = on[v] && live ? f[v][j] : 0.f;
   }
 };
 
-// Sum of one value over a row's wavefronts; `part` as for block_add.
-template <int WPR>
+// Sums over a row's LPR lanes.  Rows that span wavefronts meet at a barrier in `part`
+// (kNormThreads / 64 values that no sum before the last barrier used).
+template <int LPR>
 __device__ __forceinline__ float row_add(float v, float* part) {
-  if constexpr (WPR == 1) return wave_add(v);
-  else return block_add<WPR>(v, part);
+  if constexpr (LPR <= 64) {
+    return lanes_add<LPR>(v);
+  } else {
+    v = wave_add(v);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const float* mine = part + threadIdx.x / LPR * (LPR / 64);
+    v = mine[0];
+#pragma unroll
+    for (int i = 1; i < LPR / 64; ++i) v += mine[i];
+    return v;
+  }
 }
 
-// One row per wavefront (WPR 1, four rows a workgroup) or workgroup (WPR 4); the gain
-// and shift stay in registers over the workgroup's rows.
-template <typename X, typename Y, int E, int EPL, int WPR>
-__global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
-  using C = Cols<E, EPL, WPR>;
-  constexpr int NV = C::NV;
-  __shared__ float part[4];
-  const int tid = threadIdx.x % (64 * WPR);
+// The gain and shift stay in registers over the workgroup's rows.
+template <typename X, typename Y, int E, int EPL, int LPR>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(NormArgs a) {
+  using C = Cols<E, EPL, LPR>;
+  constexpr int NV = C::NV, RPB = kNormThreads / LPR;
+  __shared__ float part[2][2][kNormThreads / 64];
+  const int tid = threadIdx.x % LPR;
   const C c(tid, a.d);
   const float inv_d = 1.0f / (float)a.d;
   float g[NV][E], b[NV][E];
   c.load(g, a.gain);
-  if (a.shift) {
-    c.load(b, a.shift);
-  } else {
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < E; ++j) b[v][j] = 0.f;
-  }
-  for (int64_t row = (int64_t)blockIdx.x * (4 / WPR) + threadIdx.x / (64 * WPR); row < a.rows;
-       row += (int64_t)gridDim.x * (4 / WPR)) {
+  if (a.shift) c.load(b, a.shift);
+  int turn = 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+    const int64_t row = row0 + threadIdx.x / LPR;
+    const bool live = row < a.rows;  // (past the last row: it again, unstored)
+    const int64_t at = live ? row : a.rows - 1;
     float x[NV][E];
-    c.load(x, static_cast<const X*>(a.x) + row * a.ldx);
+    c.load(x, static_cast<const X*>(a.x) + at * a.ldx);
+    c.zero(x, true);
     float mu = 0.f, q = 0.f;
     if (a.norm == KF_NORM_LAYER) {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int j = 0; j < E; ++j) mu += x[v][j];
-      mu = row_add<WPR>(mu, part) * inv_d;
+      mu = row_add<LPR>(mu, part[turn][0]) * inv_d;
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -88,12 +107,17 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
         x[v][j] -= mu;
         q += c.on[v] ? x[v][j] * x[v][j] : 0.f;
       }
-    const float r = 1.0f / sqrtf(row_add<WPR>(q, part) * inv_d + a.eps);
+    const float r = 1.0f / sqrtf(row_add<LPR>(q, part[turn][1]) * inv_d + a.eps);
+    turn ^= 1;
+    if (!live) continue;
     Y* y = static_cast<Y*>(a.y) + row * a.ldy;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
 #pragma unroll
-      for (int j = 0; j < E; ++j) x[v][j] = x[v][j] * r * g[v][j] + b[v][j];
+      for (int j = 0; j < E; ++j) {
+        x[v][j] = x[v][j] * r * g[v][j];
+        if (a.shift) x[v][j] += b[v][j];
+      }
       if (c.on[v]) store_f<E>(y + c.col[v], x[v]);
     }
     if (a.stats && tid == 0) a.stats[row] = make_float2(mu, r);
@@ -101,15 +125,17 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
 }
 
 // Gradients of a strip of rows in one pass over x and dy: dx of each row, and the
-// strip's column sums in registers (a lane owns its columns), which the wavefronts of
-// a workgroup add up through LDS at the end.
-template <typename X, typename Y, int E, int EPL, int WPR, int NW>
-__global__ void __launch_bounds__(64 * NW) norm_grad_kernel(NormGradArgs a) {
-  using C = Cols<E, EPL, WPR>;
-  constexpr int NV = C::NV, RPB = NW / WPR;
-  __shared__ float part[2][NW];
-  __shared__ float sums[WPR == 1 ? NW / 2 : 1][WPR == 1 ? 2 * 64 * EPL : 1];
-  const int tid = threadIdx.x % (64 * WPR), sub = threadIdx.x / (64 * WPR);
+// strip's column sums in registers (a lane owns its columns), which the row groups of
+// a workgroup add up through LDS at the end.  Loads in flight bound it, so a lane has
+// at most 12 elements up to 4096 columns (16 a lane took 140 registers, one workgroup
+// a CU, and 204 us at 81920 x 1024 bf16 RMS, 8 take 136).
+template <typename X, typename Y, int E, int EPL, int LPR>
+__global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(NormGradArgs a) {
+  using C = Cols<E, EPL, LPR>;
+  constexpr int NV = C::NV, RPB = kNormThreads / LPR;
+  __shared__ float part[2][2][kNormThreads / 64];
+  __shared__ float sums[RPB > 1 ? RPB / 2 : 1][RPB > 1 ? 2 * EPL * LPR : 1];
+  const int tid = threadIdx.x % LPR, sub = threadIdx.x / LPR;
   const C c(tid, a.d);
   const float inv_d = 1.0f / (float)a.d;
   const bool layer = a.norm == KF_NORM_LAYER;
@@ -119,59 +145,62 @@ __global__ void __launch_bounds__(64 * NW) norm_grad_kernel(NormGradArgs a) {
   for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int j = 0; j < E; ++j) ag[v][j] = ab[v][j] = 0.f;
-  for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < a.rows; row += (int64_t)gridDim.x * RPB) {
+  int turn = 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+    const int64_t row = row0 + sub;
+    const bool live = row < a.rows;  // (past the last row: it again, with dy = 0, unstored)
+    const int64_t at = live ? row : a.rows - 1;
     float x[NV][E], dy[NV][E], res[NV][E];
-    c.load(x, static_cast<const X*>(a.x) + row * a.ldx);
-    c.load(dy, static_cast<const Y*>(a.dy) + row * a.lddy);
-    if (a.dres) {
-      c.load(res, static_cast<const X*>(a.dres) + row * a.lddres);
-    } else {
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < E; ++j) res[v][j] = 0.f;
-    }
-    const float2 st = a.stats[row];
+    c.stream(x, static_cast<const X*>(a.x) + at * a.ldx);
+    c.stream(dy, static_cast<const Y*>(a.dy) + at * a.lddy);
+    if (a.dres) c.stream(res, static_cast<const X*>(a.dres) + at * a.lddres);
+    const float2 st = a.stats[at];
+    c.zero(dy, live);
     float sw = 0.f, swx = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        x[v][j] = (x[v][j] - st.x) * st.y;  // columns past d: dy and g are zero
-        ag[v][j] += dy[v][j] * x[v][j];
+        x[v][j] = (x[v][j] - st.x) * st.y;
+        ag[v][j] += live ? dy[v][j] * x[v][j] : 0.f;  // (a NaN in the last row counts once)
         ab[v][j] += dy[v][j];
         dy[v][j] *= g[v][j];
         sw += dy[v][j];
         swx += dy[v][j] * x[v][j];
       }
-    swx = row_add<WPR>(swx, part[0]) * inv_d;
-    sw = layer ? row_add<WPR>(sw, part[1]) * inv_d : 0.f;
+    swx = row_add<LPR>(swx, part[turn][0]) * inv_d;
+    sw = layer ? row_add<LPR>(sw, part[turn][1]) * inv_d : 0.f;
+    turn ^= 1;
+    if (!live) continue;
     X* dx = static_cast<X*>(a.dx) + row * a.lddx;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
 #pragma unroll
-      for (int j = 0; j < E; ++j) x[v][j] = st.y * (dy[v][j] - sw - x[v][j] * swx) + res[v][j];
+      for (int j = 0; j < E; ++j) {
+        x[v][j] = st.y * (dy[v][j] - sw - x[v][j] * swx);
+        if (a.dres) x[v][j] += res[v][j];
+      }
       if (c.on[v]) store_f<E>(dx + c.col[v], x[v]);
     }
   }
   if (!a.part) return;
-  if constexpr (WPR == 1) {  // wavefronts in pairs: the upper half's sums to the lower half
+  if constexpr (RPB > 1) {  // row groups in pairs: the upper half's sums to the lower half
 #pragma unroll
-    for (int half = NW / 2; half > 0; half /= 2) {
+    for (int half = RPB / 2; half > 0; half /= 2) {
       __syncthreads();
       if (sub >= half && sub < 2 * half) {
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
-          sums[sub - half][i * 64 + tid] = ag[i / E][i % E];
-          sums[sub - half][(EPL + i) * 64 + tid] = ab[i / E][i % E];
+          sums[sub - half][i * LPR + tid] = ag[i / E][i % E];
+          sums[sub - half][(EPL + i) * LPR + tid] = ab[i / E][i % E];
         }
       }
       __syncthreads();
       if (sub < half) {
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
-          ag[i / E][i % E] += sums[sub][i * 64 + tid];
-          ab[i / E][i % E] += sums[sub][(EPL + i) * 64 + tid];
+          ag[i / E][i % E] += sums[sub][i * LPR + tid];
+          ab[i / E][i % E] += sums[sub][(EPL + i) * LPR + tid];
         }
       }
     }
@@ -302,26 +331,32 @@ bool vector_rows(const void* p, int64_t ld, int size, int bytes) {
   return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) % bytes == 0;
 }
 
-constexpr int kStrips = 1024;      // workgroups with column sums, at most
-constexpr int kWaveStrips = 512;   // of eight wavefronts with a row each
+constexpr int kStrips = 768;  // workgroups with column sums, at most
 
-// Rows in registers: f(E, elements a lane, wavefronts a row) as integral constants for
-// d columns (vec: vectors of 16 bytes of x), or f0() where they do not fit.
-template <int VE, typename F, typename F0>
-hipError_t by_width(int d, bool vec, F&& f, F0&& f0) {
-  auto pick = [&](auto e) {
-    constexpr int E = decltype(e)::value;
-    using std::integral_constant;
-    if (E <= 4 && d <= 64 * 4) return f(e, integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    if (d <= 64 * 8) return f(e, integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    if (E <= 4 && d <= 64 * 12) return f(e, integral_constant<int, 12>{}, integral_constant<int, 1>{});
-    if (d <= 64 * 16) return f(e, integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    if (d <= 256 * 8) return f(e, integral_constant<int, 8>{}, integral_constant<int, 4>{});
-    if (d <= 256 * 16) return f(e, integral_constant<int, 16>{}, integral_constant<int, 4>{});
-    if (d <= 256 * 32) return f(e, integral_constant<int, 32>{}, integral_constant<int, 4>{});
-    return f0();
-  };
-  return vec ? pick(std::integral_constant<int, VE>{}) : pick(std::integral_constant<int, 1>{});
+// Rows in registers: f(E, elements a lane, lanes a row) as integral constants for d
+// columns in vectors of E, or f0() where they do not fit.
+template <int E, typename F, typename F0>
+hipError_t by_width(int d, F&& f, F0&& f0) {
+  auto with = [&](auto epl, auto lpr) { return f(std::integral_constant<int, E>{}, epl, lpr); };
+#define KF_WIDTH(EPL, LPR) \
+  if (d <= EPL * LPR) return with(std::integral_constant<int, EPL>{}, std::integral_constant<int, LPR>{})
+  if constexpr (E <= 4) {
+    KF_WIDTH(4, 16);
+    KF_WIDTH(4, 32);
+    KF_WIDTH(4, 64);
+    KF_WIDTH(8, 64);
+    KF_WIDTH(12, 64);
+  } else {
+    KF_WIDTH(8, 16);
+    KF_WIDTH(8, 32);
+    KF_WIDTH(8, 64);
+  }
+  KF_WIDTH(8, 128);
+  KF_WIDTH(8, 256);
+  KF_WIDTH(8, 512);
+  KF_WIDTH(16, 512);
+#undef KF_WIDTH
+  return f0();
 }
 
 }  // namespace
@@ -334,20 +369,18 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
     const bool vec = a.d % VE == 0 && vector_rows(a.x, a.ldx, sizeof(X), 16) &&
                      vector_rows(a.y, a.ldy, sizeof(Y), VE * sizeof(Y)) && vector_rows(a.gain, 0, 4, 16) &&
                      vector_rows(a.shift, 0, 4, 16);
-    return by_width<VE>(
-        a.d, vec,
-        [&](auto e, auto epl, auto wpr) {
-          constexpr int E = decltype(e)::value, EPL = decltype(epl)::value, WPR = decltype(wpr)::value;
-          if constexpr (EPL % E == 0) {
-            const int64_t blocks = (a.rows + 4 / WPR - 1) / (4 / WPR);
-            launch((norm_kernel<X, Y, E, EPL, WPR>), dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, s, a);
-          }
-          return hipGetLastError();
-        },
-        [&] {
-          launch((norm_any_kernel<X, Y>), dim3(row_grid(a.rows)), dim3(256), 0, s, a);
-          return hipGetLastError();
-        });
+    auto rows = [&](auto e, auto epl, auto lpr) {
+      constexpr int LPR = decltype(lpr)::value, RPB = kNormThreads / LPR;
+      const int64_t blocks = (a.rows + RPB - 1) / RPB;
+      launch((norm_kernel<X, Y, decltype(e)::value, decltype(epl)::value, LPR>),
+             dim3((unsigned)(blocks < 1024 ? blocks : 1024)), dim3(kNormThreads), 0, s, a);
+      return hipGetLastError();
+    };
+    auto any = [&] {
+      launch((norm_any_kernel<X, Y>), dim3(row_grid(a.rows)), dim3(256), 0, s, a);
+      return hipGetLastError();
+    };
+    return vec ? by_width<VE>(a.d, rows, any) : by_width<1>(a.d, rows, any);
   });
 }
 
@@ -366,26 +399,25 @@ hipError_t launch_norm_grad(const NormGradArgs& args, hipStream_t s) {
       const bool vec = a.d % VE == 0 && vector_rows(a.x, a.ldx, sizeof(X), 16) &&
                        vector_rows(a.dy, a.lddy, sizeof(Y), VE * sizeof(Y)) && vector_rows(a.dx, a.lddx, sizeof(X), 16) &&
                        vector_rows(a.dres, a.dres ? a.lddres : 0, sizeof(X), 16) && vector_rows(a.gain, 0, 4, 16);
-      const hipError_t e = by_width<VE>(
-          a.d, vec,
-          [&](auto e, auto epl, auto wpr) {
-            constexpr int E = decltype(e)::value, EPL = decltype(epl)::value, WPR = decltype(wpr)::value;
-            if constexpr (EPL % E == 0) {
-              constexpr int NW = WPR == 1 ? 8 : 4, RPB = NW / WPR;
-              const int64_t blocks = (a.rows + RPB - 1) / RPB, most = WPR == 1 ? kWaveStrips : kStrips;
-              strips = (int)(blocks < most ? blocks : most);
-              launch((norm_grad_kernel<X, Y, E, EPL, WPR, NW>), dim3((unsigned)strips), dim3(64 * NW), 0, s, a);
-            }
-            return hipGetLastError();
-          },
-          [&] {
-            launch((norm_dx_any_kernel<X, Y>), dim3(row_grid(a.rows)), dim3(256), 0, s, a);
-            if (sums) {
-              strips = (int)(a.rows < 512 ? a.rows : 512);
-              launch((norm_cols_any_kernel<X, Y>), dim3((unsigned)((a.d + 255) / 256), (unsigned)strips), dim3(256), 0, s, a, strips);
-            }
-            return hipGetLastError();
-          });
+      auto rows = [&](auto e, auto epl, auto lpr) {
+        constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value, RPB = kNormThreads / LPR;
+        // as many as are resident at once
+        constexpr int most = EPL > 12 ? 256 : EPL > 8 || LPR > 64 ? 512 : kStrips;
+        const int64_t blocks = (a.rows + RPB - 1) / RPB;
+        strips = (int)(blocks < most ? blocks : most);
+        launch((norm_grad_kernel<X, Y, decltype(e)::value, EPL, LPR>), dim3((unsigned)strips),
+               dim3(kNormThreads), 0, s, a);
+        return hipGetLastError();
+      };
+      auto any = [&] {
+        launch((norm_dx_any_kernel<X, Y>), dim3(row_grid(a.rows)), dim3(256), 0, s, a);
+        if (sums) {
+          strips = (int)(a.rows < 512 ? a.rows : 512);
+          launch((norm_cols_any_kernel<X, Y>), dim3((unsigned)((a.d + 255) / 256), (unsigned)strips), dim3(256), 0, s, a, strips);
+        }
+        return hipGetLastError();
+      };
+      const hipError_t e = vec ? by_width<VE>(a.d, rows, any) : by_width<1>(a.d, rows, any);
       if (e != hipSuccess) return e;
     }
     if (sums)

@@ -31,7 +31,7 @@ def _inputs(rows, V, t, seed=0, scale=2.5):
 
 def _score(Bd, x, tok, top, where=""):
     X = x if x.is_cuda else x.cuda()
-    r = Bd.token_logprobs(X, tok.cuda(), top)
+    r = Bd.token_logprobs(X, tok.cuda(), top, lse=True)
     torch.cuda.synchronize()
     x = X.cpu()
     ref = R.logprobs(x, tok, top)
@@ -48,7 +48,7 @@ def _grad(Bd, x, tok, u, c, where="", **kw):
     X = x if x.is_cuda else x.cuda()
     dev = lambda t: None if t is None else t.cuda()
     keep = X.cpu().clone()
-    d, r = Bd.token_logprobs_backward(X, tok.cuda(), dev(u), dev(c), **kw)
+    d, r = Bd.token_logprobs_backward(X, tok.cuda(), dev(u), dev(c), entropy=True, lse=True, **kw)
     torch.cuda.synchronize()
     ref, b = R.logprobs_grad(keep, tok, u, c)
     fw = R.logprobs(keep, tok)
@@ -170,7 +170,7 @@ def test_tokens_outside_the_vocabulary(Bd):
 def test_values_that_are_not_finite(Bd):
     x, tok, u, c = _inputs(6, 1000, F32)
     x[1, 500], x[2, 0], x[4, 999] = float("nan"), math.inf, -float("nan")
-    r = Bd.token_logprobs(x.cuda(), tok.cuda(), 3)
+    r = Bd.token_logprobs(x.cuda(), tok.cuda(), 3, lse=True)
     d, _ = Bd.token_logprobs_backward(x.cuda(), tok.cuda(), u.cuda(), c.cuda())
     for i in (1, 2, 4):
         assert torch.isnan(r.logp[i]) and torch.isnan(r.entropy[i]) and torch.isnan(r.lse[i])
@@ -244,10 +244,10 @@ def test_offsets_past_32_bits(Bd):
 
 def test_same_result_on_every_run(Bd):
     x, tok, u, c = (t.cuda() for t in _inputs(700, 5003, BF))
-    a = Bd.token_logprobs(x, tok, 9)
+    a = Bd.token_logprobs(x, tok, 9, lse=True)
     d, _ = Bd.token_logprobs_backward(x, tok, u, c)
     for _ in range(3):
-        b = Bd.token_logprobs(x, tok, 9)
+        b = Bd.token_logprobs(x, tok, 9, lse=True)
         assert all(torch.equal(p, q) for p, q in zip(a, b))
         assert torch.equal(d, Bd.token_logprobs_backward(x, tok, u, c)[0])
 
@@ -256,7 +256,7 @@ def test_difference_quotient(Bd):
     """The gradient against differences of the framework's own forward pass in fp32 (error e^2 of the
     third derivative, of terms of size 8; rounding U |logp| / e)."""
     x, tok, u, c = (t.cuda() for t in _inputs(30, 400, F32))
-    d, r = Bd.token_logprobs_backward(x, tok, u, c)
+    d, r = Bd.token_logprobs_backward(x, tok, u, c, entropy=True)
     v = torch.randn(x.shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
     e = 2.0 ** -7
 
