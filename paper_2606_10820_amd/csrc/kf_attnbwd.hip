@@ -9,7 +9,7 @@
 //     kernel does; scores and dO V^T are formed transposed (keys x queries), so a
 //     lane holds one query, whose lse and D are two registers, and its dS is the B
 //     operand of dQ^T += K^T dS^T without leaving the registers.  It also forms D
-//     and stores (lse, -D) for the other walk.
+//     and stores lse / scale and D for the other walk.
 //   dK, dV: a workgroup owns 128 keys of one key region and walks the query rows
 //     that see them: at most two row intervals, the mask read by columns.  Scores
 //     are formed as queries x keys, a lane holds one key, and P and dS are the B
@@ -30,18 +30,27 @@ struct BwdArgs {
   const bf16 *Q, *K, *V, *O, *dO;
   const float* lse;
   bf16 *dQ, *dK, *dV;
-  float *lse2, *negd;  // per query row: lse in log2 units, -D
+  uint4* stats;  // per query row: lse / scale and D, each in three bf16 pieces and a zero
   int mask, N, k;
   uint32_t km;
   int nq, nk, BH;
-  float c2, scale;  // scale * log2(e), scale
+  float c2, scale, inv_scale;  // scale * log2(e), scale, 1 / scale
 };
 
-// Item t of a launch, workgroups dealt to the XCDs round-robin and each XCD given a
-// contiguous run of items (whole heads: their tiles are shared through its L2).
-__device__ inline int xcd_item(int total) {
-  const int x8 = blockIdx.x & 7, j8 = blockIdx.x >> 3;
-  return x8 * (total >> 3) + min(x8, total & 7) + j8;
+// Work order.  Heads go by groups of kGroup; within a group block j of every head, then
+// block j + 1: the heaviest blocks, numbered first, start first, and none is left to
+// start at the end.  Workgroups are dealt to the 8 XCDs round-robin, so a head's blocks
+// run on one XCD and share its tiles there (8 heads of a group; 2.6 MB of them at the
+// LM1B shape).  Head by head, dK and dV of M_D at B = 4, H = 12, N = 1024, k = 4,
+// d_head 64 took 277 us instead of 206.
+constexpr int kGroup = 64;
+struct Work {
+  int bh, j;
+};
+__device__ inline Work work_item(int t, int nb, int BH) {
+  const int first = t / (kGroup * nb) * kGroup, heads = min(kGroup, BH - first);
+  const int r = t - first * nb, j = r / heads;
+  return {first + r - j * heads, j};
 }
 
 // LDS offsets of this lane within a tile of 64 rows x DH (see Geo): natural reads
@@ -131,6 +140,13 @@ __device__ __forceinline__ void load_row(bf16x8_t (&f)[DH / 16], const bf16* row
     f[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(row + 16 * c + 8 * ((threadIdx.x & 63) >> 5)));
 }
 
+// x as the sum of three bf16 (24 bits), in the low 6 bytes.
+__device__ __forceinline__ uint2 bf16x3(float x) {
+  const bf16 a = (bf16)x, b = (bf16)(x - (float)a), c = (bf16)(x - (float)a - (float)b);
+  return make_uint2(__builtin_bit_cast(unsigned short, a) | (unsigned)__builtin_bit_cast(unsigned short, b) << 16,
+                    __builtin_bit_cast(unsigned short, c));
+}
+
 // ------------------------------------------------------------------- dQ
 template <int DH, int S, int NW>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
@@ -138,8 +154,13 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)
   using G = Geo<DH, S, NW>;
   constexpr int NC = DH / 16, NE = DH / 32, QB = 32 * NW;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S * G::STAGEB];
-  const int nqb = (a.nq + QB - 1) / QB;
-  const Item C = make_item(xcd_item(a.BH * nqb), QB, nqb, a.mask, a.N, a.k, a.km, a.nq, a.nq);
+  const int prow = a.mask == KF_MASK_DOUBLE ? a.nq / 2 : a.nq;
+  const int nqb = (prow + QB - 1) / QB * (prow < a.nq ? 2 : 1);
+  // last heads first, so that the other walk, first heads first, begins with the ones
+  // that the caches still hold; M_D's halves of rows are cut and ordered alike
+  const Work wk = work_item(blockIdx.x, nqb, a.BH);
+  const int blk = prow < a.nq ? (wk.j & 1 ? 0 : nqb / 2) + nqb / 2 - 1 - (wk.j >> 1) : nqb - 1 - wk.j;
+  const Item C = make_item((a.BH - 1 - wk.bh) * nqb + (nqb - 1 - blk), QB, nqb, a.mask, a.N, a.k, a.km, a.nq, prow);
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -168,7 +189,7 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)
   for (int j = 0; j < S - 1; ++j) issue(j, j);
 
   const int wrow = C.q0 + 32 * w, row = wrow + (lane & 31);
-  const bool valid = row < a.nq;
+  const bool valid = row < C.qe;
   const size_t grow = (size_t)C.bh * a.nq + (valid ? row : 0);
   bf16x8_t qf[NC], gf[NC];
   load_row<DH>(qf, a.Q + grow * DH);
@@ -186,12 +207,12 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)
   }
   const float l2 = a.lse[grow] * kLog2e;
   if (valid && half == 0) {
-    a.lse2[grow] = l2;
-    a.negd[grow] = nd;
+    const uint2 l = bf16x3(a.lse[grow] * a.inv_scale), d = bf16x3(-nd);
+    a.stats[grow] = make_uint4(l.x, l.y, d.x, d.y);
   }
   int wlo[3] = {0, 0, 0}, whi[3] = {0, 0, 0}, ilo[3] = {1, 1, 1}, ihi[3] = {0, 0, 0};
-  if (wrow < a.nq)
-    row_bounds(a.mask, a.N, a.k, a.km, wrow, min(wrow + 32, a.nq), wlo, whi, ilo, ihi);
+  if (wrow < C.qe)
+    row_bounds(a.mask, a.N, a.k, a.km, wrow, min(wrow + 32, C.qe), wlo, whi, ilo, ihi);
   const Intervals iv = valid ? row_intervals(a.mask, a.N, a.k, a.km, row) : no_intervals();
 
   f32x16_t dq[NE], nd16;
@@ -278,27 +299,35 @@ __device__ inline KeyRows key_rows(int mask, int N, int k, uint32_t km, int key)
   return r;
 }
 
-template <int DH, int S, int NW>
-struct KvGeo : Geo<DH, S, NW> {
-  using G = Geo<DH, S, NW>;
-  static constexpr int STAGEB = G::STAGEB + 512;  // Q tile, dO tile, lse2[64], -D[64]
-  static constexpr int PER = G::PER + 2;
+// A stage: Q tile, dO tile (64 rows each), the rows' statistics (16 bytes each).
+template <int DH, int S>
+struct KvGeo : Geo<DH, S, 4> {
+  using G = Geo<DH, S, 4>;
+  static constexpr int STAGEB = G::STAGEB + 1024;
+  static constexpr int PER = G::PER + 1;
 };
 
-template <int DH, int S, int NW>
-__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH <= 64 ? 2 : 1)))
+// Four wavefronts: KS groups of 32 keys by RS = 4 / KS groups of rows (RS 2: each takes
+// one half of every tile, and the halves' sums meet through LDS at the end).
+//
+// A row's lse and D reach all lanes of its scores as the start values of the two
+// accumulators: a matrix step with -1 over their three bf16 pieces.  Reading them from
+// LDS in the accumulators' layout was a third of the kernel's LDS traffic and 32
+// registers.
+template <int DH, int S, int KS>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 64 ? 2 : 1)))
     training_attention_dkv_kernel(BwdArgs a) {
-  using G = KvGeo<DH, S, NW>;
-  constexpr int NC = DH / 16, NE = DH / 32, KB = 32 * NW;
+  using G = KvGeo<DH, S>;
+  constexpr int NC = DH / 16, NE = DH / 32, KB = 32 * KS, RS = 4 / KS;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S * G::STAGEB];
   const int nk1 = a.N * a.k;
   // a head's key blocks: the context's (heaviest, earliest keys first), then the
   // noise blocks of each later region
   const int nb0 = (a.N + KB - 1) / KB, nb1 = (nk1 + KB - 1) / KB;
   const int nb = nb0 + (a.mask == KF_MASK_SINGLE ? 1 : 2) * nb1;
-  const int t = xcd_item(a.BH * nb);
-  const int bh = t / nb;
-  int j = t - bh * nb, r0 = 0, r1 = a.N;  // region [r0, r1) of keys
+  const Work wk = work_item(blockIdx.x, nb, a.BH);
+  const int bh = wk.bh;
+  int j = wk.j, r0 = 0, r1 = a.N;  // region [r0, r1) of keys
   if (j >= nb0) {
     j -= nb0;
     r0 = a.N;
@@ -310,7 +339,7 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
   }
   const int k0 = r0 + j * KB, ke = min(k0 + KB, r1);
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = w % KS, rg = w / KS;
 
   // the block's row tiles: its two intervals' unions, one after the other
   const KeyRows bf = key_rows(a.mask, a.N, a.k, a.km, k0), bl = key_rows(a.mask, a.N, a.k, a.km, ke - 1);
@@ -321,7 +350,7 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
   uint32_t off[G::SEGW];
 #pragma unroll
   for (int i = 0; i < G::SEGW; ++i) {
-    const int byte = (w + NW * i) * 1024 + 16 * lane;
+    const int byte = (w + 4 * i) * 1024 + 16 * lane;
     const int r = byte / G::ROWB, pc = (byte % G::ROWB) / 16;
     off[i] = r * G::ROWB + ((pc ^ swz<DH>(r)) * 16);
   }
@@ -335,17 +364,16 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     const __amdgpu_buffer_rsrc_t rg = make_rsrc(a.dO + at * DH, rows * G::ROWB);
     unsigned char* st = smem + stage * G::STAGEB;
 #pragma unroll
-    for (int i = 0; i < G::SEGW; ++i) dma16(rq, off[i], 0, st + (w + NW * i) * 1024);
+    for (int i = 0; i < G::SEGW; ++i) dma16(rq, off[i], 0, st + (w + 4 * i) * 1024);
 #pragma unroll
-    for (int i = 0; i < G::SEGW; ++i) dma16(rg, off[i], 0, st + G::TILEB + (w + NW * i) * 1024);
+    for (int i = 0; i < G::SEGW; ++i) dma16(rg, off[i], 0, st + G::TILEB + (w + 4 * i) * 1024);
     // every wavefront brings the same 64 statistics: equal load counts
-    dma4(make_rsrc(a.lse2 + at, rows * 4), 4 * lane, st + 2 * G::TILEB);
-    dma4(make_rsrc(a.negd + at, rows * 4), 4 * lane, st + 2 * G::TILEB + 256);
+    dma16(make_rsrc(a.stats + at, rows * 16), 16 * lane, 0, st + 2 * G::TILEB);
   };
 #pragma unroll
   for (int i = 0; i < S - 1; ++i) issue(i, i);
 
-  const int wkey = k0 + 32 * w, key = wkey + (lane & 31);
+  const int wkey = k0 + 32 * kg, key = wkey + (lane & 31);
   const bool valid = key < ke;
   const size_t gkey = (size_t)bh * a.nk + (valid ? key : k0);
   bf16x8_t kf[NC], vf[NC];
@@ -364,6 +392,9 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     }
   }
   if (valid) iv = key_rows(a.mask, a.N, a.k, a.km, key);
+  // -1 over the pieces of lse / scale (k-slots 0..2) and of D (8..10)
+  const bf16 m1 = (bf16)-1.f, z = (bf16)0.f, ml = half ? z : m1, md = half ? m1 : z;
+  const bf16x8_t bl8 = {ml, ml, ml, z, z, z, z, z}, bd8 = {md, md, md, z, z, z, z, z};
 
   f32x16_t dk[NE], dv[NE];
 #pragma unroll
@@ -377,42 +408,36 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     const int sg = ti >= n0;
     const int t0 = sg ? bf.lo[1] + kKT * (ti - n0) : bf.lo[0] + kKT * ti;
     const int ulo = u.lo_of(sg), uhi = u.hi_of(sg);
-    const uint32_t qb = lds_addr(smem + stage * G::STAGEB), gb = qb + G::TILEB;
-    const uint32_t sb = gb + G::TILEB + 16 * half;
+    const uint32_t base = lds_addr(smem + stage * G::STAGEB);
     stage = stage + 1 == S ? 0 : stage + 1;
-    static_for<2>([&](auto g) {
-      const int s0 = t0 + 32 * g;
+    static_for<2 / RS>([&](auto gi) {
+      const int s0 = t0 + 32 * (RS == 2 ? rg : (int)gi);
       if (s0 >= uhi || s0 + 32 <= ulo) return;  // these rows see none of the wavefront's keys
-      u32x4 qa[NC], ga[NC], l4[4], d4[4];
-      read_nat<DH, g>(qa, qb, tr);
-      read_nat<DH, g>(ga, gb, tr);
-      static_for<4>([&](auto i) {
-        l4[i] = ds_read16_off<g * 128 + i * 32>(sb);
-        d4[i] = ds_read16_off<256 + g * 128 + i * 32>(sb);
-      });
+      constexpr int G32 = RS == 2 ? 0 : (int)gi;
+      const uint32_t qb = base + (RS == 2 ? rg * 32 * G::ROWB : 0), gb = qb + G::TILEB;
+      u32x4 qa[NC], ga[NC];
+      u32x2 st = ds_read8_off<G32 * 512>(base + 2 * G::TILEB + (RS == 2 ? rg * 512 : 0) + 16 * (lane & 31) + 8 * half);
+      read_nat<DH, G32>(qa, qb, tr);
+      read_nat<DH, G32>(ga, gb, tr);
       lgkm_wait0();
-      f32x16_t s = zero16(), dp;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        pin(l4[i]);
-        pin(d4[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) dp[i] = __uint_as_float(d4[i >> 2][i & 3]);
+      pin(st);
+      const bf16x8_t sa = __builtin_bit_cast(bf16x8_t, (u32x4{st.x, st.y, 0u, 0u}));
+      f32x16_t s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sa, bl8, zero16(), 0, 0, 0);
+      f32x16_t dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sa, bd8, zero16(), 0, 0, 0);
       mul_nat<DH>(s, qa, kf);
       mul_nat<DH>(dp, ga, vf);
       u32x2 gt[2][NE][2], qt[2][NE][2];
-      read_tr<DH, g>(gt, gb, tr);
-      read_tr<DH, g>(qt, qb, tr);
+      read_tr<DH, G32>(gt, gb, tr);
+      read_tr<DH, G32>(qt, qb, tr);
       if (!(s0 >= in.lo_of(sg) && s0 + 32 <= in.hi_of(sg))) {
-        const int lo = iv.lo_of(sg), base = s0 + 4 * half - lo, width = max(iv.hi_of(sg) - lo, 0);
+        const int lo = iv.lo_of(sg), first = s0 + 4 * half - lo, width = max(iv.hi_of(sg) - lo, 0);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          s[i] = (unsigned)(base + 8 * (i >> 2) + (i & 3)) < (unsigned)width ? s[i] : -INFINITY;
+          s[i] = (unsigned)(first + 8 * (i >> 2) + (i & 3)) < (unsigned)width ? s[i] : -INFINITY;
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c2, -__uint_as_float(l4[i >> 2][i & 3])));
+        s[i] = __builtin_amdgcn_exp2f(s[i] * a.c2);
         dp[i] *= s[i];
       }
       bf16x8_t p[2], ds[2];
@@ -424,24 +449,62 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     });
   }
   vm_wait<0>();
+  if constexpr (RS == 2) {  // the second row group's sums through LDS
+    static_assert(S * G::STAGEB >= 2 * 2 * NE * 16 * 256, "room for two wavefronts' accumulators");
+    float* sums = reinterpret_cast<float*>(smem) + kg * (2 * NE * 16 * 64) + lane;
+    __syncthreads();
+    if (rg) {
+#pragma unroll
+      for (int eg = 0; eg < NE; ++eg)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sums[(eg * 16 + i) * 64] = dk[eg][i];
+          sums[((NE + eg) * 16 + i) * 64] = dv[eg][i];
+        }
+    }
+    __syncthreads();
+    if (rg) return;
+#pragma unroll
+    for (int eg = 0; eg < NE; ++eg)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        dk[eg][i] += sums[(eg * 16 + i) * 64];
+        dv[eg][i] += sums[((NE + eg) * 16 + i) * 64];
+      }
+  }
   store_row<DH>(a.dV + gkey * DH, valid, dv, 1.0f);
   store_row<DH>(a.dK + gkey * DH, valid, dk, a.scale);
 }
 
+template <int DH, int SK, int KS>
+void launch_dkv(const BwdArgs& a, hipStream_t s) {
+  constexpr int KB = 32 * KS;
+  const int nk1 = a.N * a.k;
+  const int nb = (a.N + KB - 1) / KB + (a.mask == KF_MASK_SINGLE ? 1 : 2) * ((nk1 + KB - 1) / KB);
+  launch((training_attention_dkv_kernel<DH, SK, KS>), dim3((unsigned)(a.BH * nb)), dim3(256), 0, s, a);
+}
+
+// 64 keys a workgroup, its rows in two groups, where there are few blocks of 128 context
+// keys (the long ones); 128 keys otherwise.  us of both walks, 64 | 128 keys, by the
+// number of those blocks: d_head 64 48 57 | 68, 96 154 | 186, 192 81 | 88 and 181 | 215,
+// 288 240 | 244, 384 313 | 283; d_head 32 96 26 | 30, 192 40 | 39; d_head 128 96 87 | 99,
+// 192 161 | 130.
 template <int DH, int S, int SK>
 hipError_t launch_bwd(const BwdArgs& a, hipStream_t s) {
   constexpr int NW = 4, QB = 32 * NW;
-  const int nqb = (a.nq + QB - 1) / QB, nk1 = a.N * a.k;
-  const int nb = (a.N + QB - 1) / QB + (a.mask == KF_MASK_SINGLE ? 1 : 2) * ((nk1 + QB - 1) / QB);
+  const int halves = a.mask == KF_MASK_DOUBLE ? 2 : 1, nqb = (a.nq / halves + QB - 1) / QB * halves;
   launch((training_attention_dq_kernel<DH, S, NW>), dim3((unsigned)(a.BH * nqb)), dim3(64 * NW), 0, s, a);
-  launch((training_attention_dkv_kernel<DH, SK, NW>), dim3((unsigned)(a.BH * nb)), dim3(64 * NW), 0, s, a);
+  if ((int64_t)a.BH * ((a.N + 127) / 128) <= (DH == 128 ? 96 : 192))
+    launch_dkv<DH, SK, 2>(a, s);
+  else
+    launch_dkv<DH, SK, 4>(a, s);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t training_attention_backward_bytes(int mask, int B, int H, int N, int k) {
-  return (size_t)B * H * training_attention_rows(mask, N, k) * 2 * sizeof(float);
+  return (size_t)B * H * training_attention_rows(mask, N, k) * sizeof(uint4);
 }
 
 hipError_t launch_training_attention_backward(const AttnGradArgs& g, hipStream_t s) {
@@ -464,9 +527,9 @@ hipError_t launch_training_attention_backward(const AttnGradArgs& g, hipStream_t
   if ((long long)a.nk * g.k >= (1LL << 32)) return hipErrorInvalidValue;
   a.km = g.k > 1 ? (uint32_t)(((1ULL << 32) + g.k - 1) / g.k) : 0u;
   a.BH = g.B * g.H;
-  a.lse2 = g.ws;
-  a.negd = g.ws + (size_t)a.BH * a.nq;
+  a.stats = reinterpret_cast<uint4*>(g.ws);
   a.scale = g.scale;
+  a.inv_scale = 1.0f / g.scale;
   a.c2 = g.scale * kLog2e;
   switch (g.dh) {
     case 32: return launch_bwd<32, 3, 2>(a, s);
