@@ -336,8 +336,8 @@ int kf_training_attention(void *hip_stream, int mask, int B, int H, int N, int k
 
 /* kf_training_attention that also keeps, for the backward pass, each query
  * row's natural log of the sum of exp(scale * q.k) over its visible keys:
- * lse fp32 [B][H][rows].  O is kf_training_attention's bit for bit.  scale > 0,
- * and keys * k below 2^32. */
+ * lse fp32 [B][H][rows].  O is kf_training_attention's bit for bit.  scale in
+ * [1e-20, 1e20], keys * k below 2^32 (else KF_EINVAL). */
 int kf_training_attention_lse(void *hip_stream, int mask, int B, int H, int N, int k, int d_head,
                               const void *Q, const void *K, const void *V, void *O, float *lse,
                               float scale);
@@ -351,7 +351,7 @@ int kf_training_attention_lse(void *hip_stream, int mask, int B, int H, int N, i
  * P and dS are rounded to bf16 for the matrix products, all sums are fp32 and
  * of a fixed order (no atomics: a call's result is the same on every run).
  * Inputs are finite: an infinity or NaN may spread to rows and keys of its head
- * that do not see it.  scale > 0, and keys * k below 2^32.
+ * that do not see it.  scale in [1e-20, 1e20], keys * k below 2^32.
  * workspace: kf_training_attention_backward_bytes() bytes of device memory,
  * 16-byte aligned, used during the call only; calls that overlap need one
  * each.  The size is 0 for arguments that the call refuses and for an empty
@@ -370,7 +370,8 @@ int kf_training_attention_backward(void *hip_stream, int mask, int B, int H, int
  * stream) of the calling thread's current device, nothing allocated, nothing
  * copied from or to the host, no clearing by the runtime (a call can be
  * captured into a HIP graph), KF_EINVAL before any launch for a bad argument,
- * KF_EHIP when a launch fails.  Sums have a fixed order: no atomics.  Types:
+ * KF_EHIP when a launch fails.  Sums have a fixed order: results are the same
+ * on every run.  Types:
  * KF_FP32, KF_BF16 and KF_FP16, rounded to nearest even where a result is
  * stored, statistics and sums in fp32 (the gradient norm in fp64).  Pointers
  * are aligned to their element.  Rows are d (or vocab) consecutive elements,
@@ -446,7 +447,8 @@ int kf_token_logprobs_backward(void *hip_stream, int dtype, int64_t rows, int vo
  * tensors.  Each holds n consecutive elements src of src_dtype; the scaled
  * gradient goes to dst: of the same type, or fp32 (half-precision gradients
  * into an fp32 optimiser's).  dst may be src (same type) or null in a plan
- * that only kf_grad_norm uses; other overlaps are not allowed. */
+ * that only kf_grad_norm uses; a dst that overlaps another dst or another src
+ * is KF_EINVAL (a tensor listed twice in place would be scaled twice). */
 typedef struct kf_grad {
   const void *src;
   void *dst;

@@ -318,11 +318,13 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
 #pragma unroll
         for (int k = 0; k < NW; ++k) v = fmaxf(v, sh.lane_max[64 * k + lane]);
       }
+      // Where fewer than n sets hold a finite logit (a vocabulary masked down to a few
+      // ids), the finite ones are offered and, of the others, the ids below n: there are
+      // enough of them.
       auto reach = [&](float b) { return __popcll(__builtin_amdgcn_ballot_w64(v >= b)) >= n; };
       float bound = fmaxf(wave_min(v), -3.4028235e38f), hi = m;
-      if (!reach(bound)) {
-        bound = -INFINITY;
-      } else {
+      const bool few = !reach(bound);
+      if (!few) {
 #pragma unroll 1
         for (int k = 0; k < 10; ++k) {
           const float mid = 0.5f * bound + 0.5f * hi;
@@ -330,12 +332,14 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
           else hi = mid;
         }
       }
+      auto put = [&](float f, int id) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kTopCap) sh.key[at] = top_key(f, id);
+      };
+      if (few && tid < n && (float)x[tid] < bound) put((float)x[tid], tid);
       if (s == s && __builtin_amdgcn_ballot_w64(tm >= bound)) {
         auto offer = [&](float f, int id) {
-          if (f >= bound) {
-            const int at = atomicAdd(&sh.count, 1);
-            if (at < kTopCap) sh.key[at] = top_key(f, id);
-          }
+          if (f >= bound) put(f, id);
         };
         if (edge >= 0) offer(ex, edge);
         auto offer_all = [&](const u32x4& q, int k) {

@@ -1,6 +1,7 @@
 // kf_train_api.cpp -- C entries of the training step's operators: argument checks,
 // then the launches of kf_norm.hip, kf_logprobs.hip and kf_clip.hip.
 #include <math.h>
+#include <stdlib.h>
 
 #include "kforcing.h"
 #include "kf_train.h"
@@ -32,6 +33,41 @@ bool grad_ok(const kf_grad& g) {
   return aligned(g.src, sb) && aligned_or_null(g.dst, db) &&
          !(g.dst == g.src && g.src_dtype != g.dst_dtype);
 }
+
+// Whether a destination overlaps another tensor's or any source but its own: then the
+// order of workgroups would decide.  Sorts the address ranges; a range is one end of
+// memory (no C++ container: nothing here may throw).
+struct Range {
+  uintptr_t lo, hi;
+  int dst;
+};
+int by_lo(const void* a, const void* b) {
+  const uintptr_t x = static_cast<const Range*>(a)->lo, y = static_cast<const Range*>(b)->lo;
+  return x < y ? -1 : x > y;
+}
+int overlaps(int n, const kf_grad* g) {  // 1, 0, or -1 for want of memory
+  if (n == 0) return 0;
+  Range* r = static_cast<Range*>(malloc(sizeof(Range) * 2 * (size_t)n));
+  if (!r) return -1;
+  size_t m = 0;
+  auto add = [&](const void* p, int64_t bytes, int dst) {
+    if (p && bytes) r[m++] = {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, dst};
+  };
+  for (int i = 0; i < n; ++i) {
+    add(g[i].dst, g[i].n * type_bytes(g[i].dst_dtype), 1);
+    if (g[i].dst != g[i].src) add(g[i].src, g[i].n * type_bytes(g[i].src_dtype), 0);
+  }
+  qsort(r, m, sizeof(Range), by_lo);
+  uintptr_t any = 0, dst = 0;  // where the ranges so far end
+  int bad = 0;
+  for (size_t i = 0; i < m && !bad; ++i) {
+    bad = r[i].lo < (r[i].dst ? any : dst);
+    if (r[i].hi > any) any = r[i].hi;
+    if (r[i].dst && r[i].hi > dst) dst = r[i].hi;
+  }
+  free(r);
+  return bad;
+}
 constexpr size_t kPartBytes = (size_t)kf::kGradPartials * sizeof(double);
 kf::GradChunk* plan_table(const kf_grad_plan* p) {
   return reinterpret_cast<kf::GradChunk*>(static_cast<char*>(p->dev) + kPartBytes);
@@ -61,9 +97,9 @@ int kf::check_training_attention(int mask, int B, int H, int N, int k, int d_hea
 namespace {
 // The limits of the calls with gradients: q / k by a reciprocal, workgroups of both
 // walks; a scale of zero or less turns a masked score, minus infinity, into NaN or a
-// maximum.
+// maximum, and lse / scale is stored.
 bool attn_grad_fits(int mask, int B, int H, int N, int k, float scale) {
-  if (!(scale > 0.f)) return false;
+  if (!(scale >= 1e-20f && scale <= 1e20f)) return false;
   const int64_t nk = (int64_t)N * k, keys = mask == KF_MASK_SINGLE ? N + nk : N + 2 * nk;
   return keys * k < ((int64_t)1 << 32) && (int64_t)B * H * (keys / 32 + 4) < ((int64_t)1 << 31);
 }
@@ -206,6 +242,8 @@ int kf_grad_plan_init(void* hip_stream, int n, const kf_grad* grads, void* dev, 
                       kf_grad_plan* plan) {
   const size_t need = kf_grad_plan_bytes(n, grads);
   if (!need || bytes < need || !plan || !aligned(dev, 256)) return KF_EINVAL;
+  const int rc_overlap = overlaps(n, grads);
+  if (rc_overlap) return rc_overlap < 0 ? KF_ENOMEM : KF_EINVAL;
   kf_grad_plan p = {dev, kf::grad_chunks(n, grads), 1};
   if (p.chunks >= ((int64_t)1 << 31)) return KF_EINVAL;
   for (int i = 0; i < n; ++i)

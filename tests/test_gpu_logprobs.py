@@ -142,6 +142,24 @@ def test_ties_go_to_the_lowest_id(Bd, V, t):
         _score(Bd, x.to(t), torch.zeros(8, dtype=torch.int32), top, f"ties top {top}")
 
 
+def test_few_unmasked_ids(Bd):
+    """Fewer finite logits than alternatives, at the start, the end and within, one lane's or all lanes';
+    the rest are the lowest masked ids."""
+    for t in TYPES:
+        for V in (65, 300, 5000, 50257):
+            x = torch.full((8, V), -math.inf)
+            x[0, 0] = 1.0
+            x[1, V - 1] = 1.0
+            x[2, [1, 3, V // 2]] = torch.tensor([0.5, 0.5, 2.0])
+            x[3, ::max(1, V // 5)] = -1.0
+            x[4, 2:40] = torch.arange(38).float()
+            x[5, torch.arange(0, V, 64)[:60]] = 3.0
+            x[7, : min(V, 64)] = 0.25
+            tok = torch.zeros(8, dtype=torch.int32)
+            for top in (1, 5, 20, 64):
+                _score(Bd, x.to(t), tok, top, f"few V {V} top {top}")
+
+
 def test_sorted_clusters(Bd):
     """The largest logits next to each other, and a stride apart: they fall to few lanes, or one."""
     for V in (5000, 50257):

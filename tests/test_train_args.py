@@ -96,6 +96,11 @@ def test_clip_refusals(L):
     assert L.kf_grad_plan_init(None, 1, arr(good), A, n - 1, ctypes.byref(plan)) == Bd.KF_EINVAL
     assert L.kf_grad_plan_init(None, 1, arr(good), P(0x10010), n, ctypes.byref(plan)) == Bd.KF_EINVAL
     assert L.kf_grad_plan_init(None, 1, arr(good), A, n, None) == Bd.KF_EINVAL
+    # a dst on another dst, on another src, half over its own src, a tensor twice in place
+    for clash in ((good, (0x30000, 0x20010, 10, 0, 0)), (good, (0x30000, 0x10020, 4, 0, 0)), ((0x10000, 0x10010, 10, 0, 0),),
+                  ((0x10000, 0x10000, 10, 0, 0),) * 2):
+        a = arr(*clash)
+        assert L.kf_grad_plan_init(None, len(clash), a, A, 1 << 30, ctypes.byref(plan)) == Bd.KF_EINVAL, clash
     fake = Bd.KfGradPlan(0x10000, 1, 1)
     assert L.kf_grad_norm(None, None, A) == Bd.KF_EINVAL
     assert L.kf_grad_norm(None, ctypes.byref(fake), None) == Bd.KF_EINVAL
@@ -116,7 +121,7 @@ def test_attention_backward_refusals(L):
         a = dict(ok, **kw)
         return L.kf_training_attention_backward(None, a["mask"], a["B"], a["H"], a["N"], a["k"], a["dh"], *ptrs, a["scale"], ws, n)
 
-    for bad in (dict(mask=2), dict(k=0), dict(B=-1), dict(N=-3), dict(dh=48), dict(scale=INF), dict(scale=NAN), dict(scale=0.0), dict(scale=-0.2),
+    for bad in (dict(mask=2), dict(k=0), dict(B=-1), dict(N=-3), dict(dh=48), dict(scale=INF), dict(scale=NAN), dict(scale=0.0), dict(scale=-0.2), dict(scale=1e-21), dict(scale=1e21),
                 dict(mask=1, N=1 << 22, k=4), dict(N=4000, k=2000, dh=32, B=1, H=1)):
         assert fwd(**bad) == Bd.KF_EINVAL, bad
         assert bwd(**bad) == Bd.KF_EINVAL, bad
