@@ -128,7 +128,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(NormArgs a) {
 // strip's column sums in registers (a lane owns its columns), which the row groups of
 // a workgroup add up through LDS at the end.  Loads in flight bound it, so a lane has
 // at most 12 elements up to 4096 columns (16 a lane took 140 registers, one workgroup
-// a CU, and 204 us at 81920 x 1024 bf16 RMS, 8 take 136).
+// a CU, and 204 us at 81920 x 1024 bf16 RMS; 8 take 110, 6.1 TB/s).  dy and dres are
+// streamed past the caches, x is not, whose forward pass may be near (forward and
+// backward at 40960 x 768, fp32 in, bf16 out: x streamed too 124 us, all kept 118,
+// this 113; 81920 x 1024 187, 188, 178).
 template <typename X, typename Y, int E, int EPL, int LPR>
 __global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(NormGradArgs a) {
   using C = Cols<E, EPL, LPR>;
@@ -151,7 +154,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(NormGradArgs a)
     const bool live = row < a.rows;  // (past the last row: it again, with dy = 0, unstored)
     const int64_t at = live ? row : a.rows - 1;
     float x[NV][E], dy[NV][E], res[NV][E];
-    c.stream(x, static_cast<const X*>(a.x) + at * a.ldx);
+    c.load(x, static_cast<const X*>(a.x) + at * a.ldx);
     c.stream(dy, static_cast<const Y*>(a.dy) + at * a.lddy);
     if (a.dres) c.stream(res, static_cast<const X*>(a.dres) + at * a.lddres);
     const float2 st = a.stats[at];
