@@ -18,16 +18,15 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Order of the alternatives: larger logits first, equal ones by the lower id; NaN
 // before everything, and -0 equal to 0.
-__device__ __forceinline__ unsigned long long top_key(float x, int id) {
-  unsigned b = __float_as_uint(x + 0.0f);
-  b = b & 0x80000000u ? ~b : b | 0x80000000u;
-  if (x != x) b = 0xFFFFFFFFu;
-  return (unsigned long long)b << 32 | (unsigned)~id;
+__device__ __forceinline__ unsigned order_of(float x) {
+  const unsigned b = __float_as_uint(x + 0.0f);
+  return x != x ? 0xFFFFFFFFu : b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-
-// The logit of a key (0 for -0; not for NaN).
-__device__ __forceinline__ float key_value(unsigned long long key) {
-  const unsigned b = (unsigned)(key >> 32);
+__device__ __forceinline__ unsigned long long top_key(float x, int id) {
+  return (unsigned long long)order_of(x) << 32 | (unsigned)~id;
+}
+// The logit of an order (0 for -0; not for NaN).
+__device__ __forceinline__ float logit_of(unsigned b) {
   return __uint_as_float(b & 0x80000000u ? b & 0x7FFFFFFFu : ~b);
 }
 
@@ -127,7 +126,8 @@ constexpr int kTopCap = 256;  // alternatives' candidates kept in LDS
 // One row's LDS.
 template <int NT>
 struct RowShared {
-  float m[NT / 64], s[NT / 64], w[NT / 64];
+  static constexpr int NW = NT < 64 ? 1 : NT / 64;
+  float m[NW], s[NW], w[NW];
   float lane_max[NT];
   int count;
   unsigned long long key[kTopCap];
@@ -155,9 +155,11 @@ template <typename T, int NT, int NV, bool GRAD>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_waves_per_eu(row_waves(NT, NV))))
     logprobs_kernel(LogprobArgs a) {
   using R = Raw<T>;
-  constexpr int E = R::E, RPB = NT < 256 ? 256 / NT : 1, NW = NT / 64, NR = NV ? NV : 4;
-  __shared__ RowShared<NT> shared[RPB];
-  RowShared<NT>& sh = shared[threadIdx.x / NT];
+  constexpr int E = R::E, RPB = NT < 256 ? 256 / NT : 1, NW = NT < 64 ? 1 : NT / 64, NR = NV ? NV : 4;
+  constexpr int NL = NT < 64 ? NT : 64;  // lanes of one wavefront that share a row
+  constexpr bool kTop = !GRAD && NT >= 64;
+  __shared__ RowShared<NT> shared[kTop || NW > 1 ? RPB : 1];
+  RowShared<NT>& sh = shared[kTop || NW > 1 ? threadIdx.x / NT : 0];
   const int tid = threadIdx.x % NT, lane = tid & 63, V = a.vocab;
   const int wv = __builtin_amdgcn_readfirstlane(tid & ~63);  // the wavefront's first thread
   const int64_t step = (int64_t)gridDim.x * RPB;
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
 #pragma unroll
         for (int i = 0; i < E; ++i) tm = fmaxf(tm, R::get(q, i));
       }, false);
-      m = wave_max(tm);
+      m = lanes_max<NL>(tm);
       mr = m == -INFINITY ? 0.f : m;
       s = w = 0.f;
       sum(ex);
@@ -241,9 +243,9 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
       m = wave_max(tm);
       rebase(tm, m);
     }
-    s = wave_add(s);
-    w = wave_add(w);
-    const bool top = !GRAD && a.n_top > 0;
+    s = lanes_add<NL>(s);
+    w = lanes_add<NL>(w);
+    const bool top = kTop && a.n_top > 0;
     if constexpr (NW > 1) {  // the wavefronts' results joined, the same in every one
       if (lane == 0) {
         sh.m[tid >> 6] = m;
@@ -306,89 +308,99 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
           for (int i = 0; i < E; ++i) to[i] = (T)d[i];
         }
       });
-    } else if (top) {
-      // Alternatives.  The 64 lanes (of all wavefronts) hold 64 sets of elements; a
-      // bound that n_top of the sets' maxima reach is one that the n_top largest
-      // elements reach.  The elements that reach it, few beyond n_top, are ranked
-      // against each other.  A row with NaN or plus infinity (s is NaN) or with too many
-      // of them (equal logits) goes the long way.
-      const int n = a.n_top;
-      float v = tm;
-      if constexpr (NW > 1) {
+    } else if constexpr (kTop) {
+      if (top) {
+        // Alternatives.  The 64 lanes (of all wavefronts) hold 64 sets of elements; a
+        // bound that n_top of the sets' maxima reach is one that the n_top largest
+        // elements reach.  The elements that reach it, few beyond n_top, are ranked
+        // against each other.  A row with NaN or plus infinity (s is NaN) or with too many
+        // of them (equal logits) goes the long way.
+        const int n = a.n_top;
+        float v = tm;
+        if constexpr (NW > 1) {
 #pragma unroll
-        for (int k = 0; k < NW; ++k) v = fmaxf(v, sh.lane_max[64 * k + lane]);
-      }
-      // Where fewer than n sets hold a finite logit (a vocabulary masked down to a few
-      // ids), the finite ones are offered and, of the others, the ids below n: there are
-      // enough of them.
-      auto reach = [&](float b) { return __popcll(__builtin_amdgcn_ballot_w64(v >= b)) >= n; };
-      float bound = fmaxf(wave_min(v), -3.4028235e38f), hi = m;
-      const bool few = !reach(bound);
-      if (!few) {
-#pragma unroll 1
-        for (int k = 0; k < 10; ++k) {
-          const float mid = 0.5f * bound + 0.5f * hi;
-          if (reach(mid)) bound = mid;
-          else hi = mid;
+          for (int k = 0; k < NW; ++k) v = fmaxf(v, sh.lane_max[64 * k + lane]);
         }
-      }
-      auto put = [&](float f, int id) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < kTopCap) sh.key[at] = top_key(f, id);
-      };
-      if (few && tid < n && (float)x[tid] < bound) put((float)x[tid], tid);
-      if (s == s && __builtin_amdgcn_ballot_w64(tm >= bound)) {
-        auto offer = [&](float f, int id) {
-          if (f >= bound) put(f, id);
+        // Where fewer than n sets hold a finite logit (a vocabulary masked down to a few
+        // ids), the finite ones are offered and, of the others, the ids below n: there are
+        // enough of them.
+        // The bound is found by halving between the sets' least finite maximum and the
+        // row's maximum, in the order of the float32 bits, until n of the sets reach it.
+        const unsigned mine = order_of(v);
+        auto reaching = [&](unsigned b) { return __popcll(__builtin_amdgcn_ballot_w64(mine >= b)); };
+        unsigned lo = order_of(fmaxf(wave_min(v == -INFINITY ? INFINITY : v), -3.4028235e38f)), hi = order_of(m);
+        int c = reaching(lo);
+        const bool few = c < n || m == -INFINITY;
+#pragma unroll 1
+        for (int k = 0; k < 12 && c > n && lo + 1 < hi; ++k) {
+          const unsigned mid = lo + (hi - lo) / 2;
+          const int d = reaching(mid);
+          if (d >= n) {
+            lo = mid;
+            c = d;
+          } else {
+            hi = mid;
+          }
+        }
+        const float bound = few ? -3.4028235e38f : logit_of(lo);
+        auto put = [&](float f, int id) {
+          const int at = atomicAdd(&sh.count, 1);
+          if (at < kTopCap) sh.key[at] = top_key(f, id);
         };
-        if (edge >= 0) offer(ex, edge);
-        auto offer_all = [&](const u32x4& q, int k) {
+        if (few && tid < n && (float)x[tid] < bound) put((float)x[tid], tid);
+        if (s == s && __builtin_amdgcn_ballot_w64(tm >= bound)) {
+          auto offer = [&](float f, int id) {
+            if (f >= bound) put(f, id);
+          };
+          if (edge >= 0) offer(ex, edge);
+          auto offer_all = [&](const u32x4& q, int k) {
 #pragma unroll
-          for (int i = 0; i < E; ++i) offer(R::get(q, i), head + k * E + i);
-        };
-        if constexpr (NV > 0) {
-          each([&](const u32x4& q, int k) {
-            if (k < nb && tm >= bound) offer_all(q, k);
-          });
-        } else {
-          // read again, all lanes together: a thread's vectors whose maximum reaches it
-          unsigned long long who = __builtin_amdgcn_ballot_w64(tm >= bound);
-          while (who) {
-            int of[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              of[j] = who ? wv + __builtin_ctzll(who) : nb;
-              who &= who - 1;
-            }
-            for (int i = lane * NT; i < nb; i += 64 * NT) {
+            for (int i = 0; i < E; ++i) offer(R::get(q, i), head + k * E + i);
+          };
+          if constexpr (NV > 0) {
+            each([&](const u32x4& q, int k) {
+              if (k < nb && tm >= bound) offer_all(q, k);
+            });
+          } else {
+            // read again, all lanes together: a thread's vectors whose maximum reaches it
+            unsigned long long who = __builtin_amdgcn_ballot_w64(tm >= bound);
+            while (who) {
+              int of[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                r[j] = u32x4{R::kFill, R::kFill, R::kFill, R::kFill};
-                if (of[j] + i < nb) r[j] = xv[of[j] + i];
+                of[j] = who ? wv + __builtin_ctzll(who) : nb;
+                who &= who - 1;
               }
+              for (int i = lane * NT; i < nb; i += 64 * NT) {
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (of[j] + i < nb) offer_all(r[j], of[j] + i);
+                for (int j = 0; j < 4; ++j) {
+                  r[j] = u32x4{R::kFill, R::kFill, R::kFill, R::kFill};
+                  if (of[j] + i < nb) r[j] = xv[of[j] + i];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (of[j] + i < nb) offer_all(r[j], of[j] + i);
+              }
             }
           }
         }
-      }
-      row_sync<NT>();
-      const int count = sh.count;
-      if (s == s && count <= kTopCap) {
-        for (int i = tid; i < count; i += NT) {
-          const unsigned long long key = sh.key[i];
-          int rank = 0;
+        row_sync<NT>();
+        const int count = sh.count;
+        if (s == s && count <= kTopCap) {
+          for (int i = tid; i < count; i += NT) {
+            const unsigned long long key = sh.key[i];
+            int rank = 0;
 #pragma unroll 4
-          for (int k = 0; k < count; ++k) rank += sh.key[k] > key;
-          if (rank < n) {
-            a.top_ids[row * n + rank] = (int)~(unsigned)key;
-            a.top_logp[row * n + rank] = empty ? -INFINITY : (key_value(key) - mr) - ls;
+            for (int k = 0; k < count; ++k) rank += sh.key[k] > key;
+            if (rank < n) {
+              a.top_ids[row * n + rank] = (int)~(unsigned)key;
+              a.top_logp[row * n + rank] = empty ? -INFINITY : (logit_of((unsigned)(key >> 32)) - mr) - ls;
+            }
           }
+        } else {
+          row_sync<NT>();  // the keys make room
+          top_rounds<T, NT>(a, row, x, tid, mr, ls, empty, sh.key);
         }
-      } else {
-        row_sync<NT>();  // the keys make room
-        top_rounds<T, NT>(a, row, x, tid, mr, ls, empty, sh.key);
       }
     }
     if (NW > 1 && row + step < a.rows) __syncthreads();  // the next row's LDS
@@ -405,10 +417,6 @@ hipError_t by_type(int dtype, F&& f) {
   }
 }
 
-}  // namespace
-
-namespace {
-
 template <typename T, int NT, int NV, bool GRAD>
 hipError_t launch_rows(const LogprobArgs& a, hipStream_t s) {
   constexpr int RPB = NT < 256 ? 256 / NT : 1;
@@ -418,7 +426,9 @@ hipError_t launch_rows(const LogprobArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Threads, and vectors a thread holds, by a row's 16-byte vectors.  The gradient needs a
+// Threads, and vectors a thread holds, by a row's 16-byte vectors.  Narrow rows without
+// alternatives share a wavefront, 16 or 32 lanes each (1171875 x 128 bf16 412 -> 88 us,
+// gradient 515 -> 149).  The gradient needs a
 // row twice, so a row stays in registers as long as they hold it; the sums alone stream
 // it from 2049 vectors on, which keeps more rows in flight.  us, plain | with 8
 // alternatives, held in registers and streamed in 256, 512, 1024 threads:
@@ -429,6 +439,8 @@ hipError_t launch_rows(const LogprobArgs& a, hipStream_t s) {
 template <typename T, bool GRAD>
 hipError_t launch_by_width(const LogprobArgs& a, hipStream_t s) {
   const int nv = a.vocab / Raw<T>::E;
+  if (!a.n_top && nv <= 16) return launch_rows<T, 16, 1, GRAD>(a, s);
+  if (!a.n_top && nv <= 32) return launch_rows<T, 32, 1, GRAD>(a, s);
   if (nv <= 64) return launch_rows<T, 64, 1, GRAD>(a, s);
   if (nv <= 128) return launch_rows<T, 64, 2, GRAD>(a, s);
   if (nv <= 256) return launch_rows<T, 64, 4, GRAD>(a, s);

@@ -106,12 +106,14 @@ template <int N>
 __device__ __forceinline__ float lanes_add(float v) {
   return lanes_reduce<N>(v, [](float a, float b) { return a + b; });
 }
+template <int N>
+__device__ __forceinline__ float lanes_max(float v) {  // a NaN yields to a number
+  return lanes_reduce<N>(v, [](float a, float b) { return fmaxf(a, b); });
+}
 __device__ __forceinline__ float wave_add(float v) {
   return lanes_add<64>(v);
 }
-__device__ __forceinline__ float wave_max(float v) {  // a NaN yields to a number
-  return lanes_reduce<64>(v, [](float a, float b) { return fmaxf(a, b); });
-}
+__device__ __forceinline__ float wave_max(float v) { return lanes_max<64>(v); }
 __device__ __forceinline__ float wave_min(float v) {
   return lanes_reduce<64>(v, [](float a, float b) { return fminf(a, b); });
 }
