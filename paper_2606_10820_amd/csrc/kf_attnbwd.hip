@@ -11,17 +11,21 @@
 //     operand of dQ^T += K^T dS^T without leaving the registers.  It also forms D
 //     and stores lse / scale and D for the other walk.  D = dO.O carries the roundings
 //     of O and of the forward pass's P (bf16: up to 2^-8 each); the exact D is the one
-//     that makes a row of dS sum to zero, so with e the fp32 sum of that row before its
-//     rounding to bf16, D + e is stored and dQ becomes dQ - scale e (P K), for one more
-//     product.  (Error of dQ and dK against 64 bits, norms, N = 16, k = 4: 2.8e-3 and
-//     2.7e-3 without, 2.4e-3 with, of which 1.7e-3 are the results' own rounding; M_D at
-//     N = 1024 380 -> 407 us forward and backward.)
+//     that makes a row of dS sum to zero, so D + (the fp32 sum of that row) is stored.
+//     dS enters the product as two bf16 terms, its rounding and the rest: one product
+//     more, and less time than taking D's error out of dQ (32 registers for P K, two
+//     wavefronts per SIMD instead of three: 171 us against 154).
 //   dK, dV: a workgroup owns 128 keys of one key region and walks the query rows
 //     that see them: at most two row intervals, the mask read by columns.  Scores
 //     are formed as queries x keys, a lane holds one key, and P and dS are the B
 //     operands of dV^T += dO^T P and dK^T += Q^T dS.
-// Together they form scores and dO V^T twice: 8 products of the visible pairs, where a
-// single walk that adds dQ with atomics would form 5.
+// On small grids (FINE) P and dS enter dV and dK as two terms as well.  Errors against 64
+// bits (norms; the results' own rounding is 1.7e-3): dQ 1.8e-3 to 2.2e-3, dK and dV
+// 2.4e-3, on small grids 1.8e-3.  One term everywhere and D as it comes took dQ and dK to
+// 2.5e-3 to 2.8e-3; two terms everywhere take dK and dV of M_D at N = 1024 from 209 to
+// 270 us.
+// Together the walks form scores and dO V^T twice: 8 products of the visible pairs, where
+// a single walk that adds dQ with atomics would form 5 or 6.
 // Operands that a product needs with the other index first come through the
 // transposing LDS reads of the same tiles.
 #include "kf_blockattn.h"
@@ -139,6 +143,18 @@ __device__ __forceinline__ void to_bf16(bf16x8_t (&d)[2], const f32x16_t& s) {
       d[j][r + 1] = h[1];
     }
 }
+// What that rounding left, s - d, in bf16 again.
+__device__ __forceinline__ void rest_bf16(bf16x8_t (&l)[2], const f32x16_t& s, const bf16x8_t (&d)[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int r = 0; r < 8; r += 2) {
+      const f32x2_t e = {s[8 * j + r] - (float)d[j][r], s[8 * j + r + 1] - (float)d[j][r + 1]};
+      const bf16x2_t h = __builtin_convertvector(e, bf16x2_t);
+      l[j][r] = h[0];
+      l[j][r + 1] = h[1];
+    }
+}
 template <int DH>
 __device__ __forceinline__ void load_row(bf16x8_t (&f)[DH / 16], const bf16* row) {
 #pragma unroll
@@ -155,7 +171,7 @@ __device__ __forceinline__ uint2 bf16x3(float x) {
 
 // ------------------------------------------------------------------- dQ
 template <int DH, int S, int NW>
-__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH <= 64 ? 2 : 1)))
+__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH <= 64 ? 3 : 2)))
     training_attention_dq_kernel(BwdArgs a) {
   using G = Geo<DH, S, NW>;
   constexpr int NC = DH / 16, NE = DH / 32, QB = 32 * NW;
@@ -217,10 +233,10 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     row_bounds(a.mask, a.N, a.k, a.km, wrow, min(wrow + 32, C.qe), wlo, whi, ilo, ihi);
   const Intervals iv = valid ? row_intervals(a.mask, a.N, a.k, a.km, row) : no_intervals();
 
-  f32x16_t dq[NE], pk[NE], nd16;
+  f32x16_t dq[NE], nd16;
   float eps = 0.f;  // this half's part of the row sum of dS
 #pragma unroll
-  for (int eg = 0; eg < NE; ++eg) dq[eg] = pk[eg] = zero16();
+  for (int eg = 0; eg < NE; ++eg) dq[eg] = zero16();
 #pragma unroll
   for (int i = 0; i < 16; ++i) nd16[i] = nd;
 
@@ -261,12 +277,12 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
 #pragma unroll
       for (int i = 1; i < 16; ++i) part += dp[i];
       eps += part;
-      bf16x8_t p[2], ds[2];
-      to_bf16(p, s);
+      bf16x8_t ds[2], rest[2];
       to_bf16(ds, dp);
+      rest_bf16(rest, dp, ds);
       lgkm_wait0();
       mul_tr<DH>(dq, kt, ds);
-      mul_tr<DH>(pk, kt, p);
+      mul_tr<DH>(dq, kt, rest);
     });
   }
   vm_wait<0>();  // loads issued for tiles past the last one
@@ -274,10 +290,6 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(eps), __float_as_uint(eps), false, false);
     eps = __uint_as_float(both[0]) + __uint_as_float(both[1]);
   }
-#pragma unroll
-  for (int eg = 0; eg < NE; ++eg)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) dq[eg][i] -= eps * pk[eg][i];
   if (valid && half == 0) {
     const uint2 l = bf16x3(a.lse[grow] * a.inv_scale), d = bf16x3(eps - nd);
     a.stats[grow] = make_uint4(l.x, l.y, d.x, d.y);
@@ -338,7 +350,7 @@ struct KvGeo : Geo<DH, S, 4> {
 // accumulators: a matrix step with -1 over their three bf16 pieces.  Reading them from
 // LDS in the accumulators' layout was a third of the kernel's LDS traffic and 32
 // registers.
-template <int DH, int S, int KS>
+template <int DH, int S, int KS, bool FINE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 64 ? 2 : 1)))
     training_attention_dkv_kernel(BwdArgs a) {
   using G = KvGeo<DH, S>;
@@ -470,6 +482,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 
       lgkm_wait0();
       mul_tr<DH>(dv, gt, p);
       mul_tr<DH>(dk, qt, ds);
+      if constexpr (FINE) {
+        bf16x8_t rest[2];
+        rest_bf16(rest, s, p);
+        mul_tr<DH>(dv, gt, rest);
+        rest_bf16(rest, dp, ds);
+        mul_tr<DH>(dk, qt, rest);
+      }
     });
   }
   vm_wait<0>();
@@ -500,12 +519,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 
   store_row<DH>(a.dK + gkey * DH, valid, dk, a.scale);
 }
 
-template <int DH, int SK, int KS>
+template <int DH, int SK, int KS, bool FINE>
 void launch_dkv(const BwdArgs& a, hipStream_t s) {
   constexpr int KB = 32 * KS;
   const int nk1 = a.N * a.k;
   const int nb = (a.N + KB - 1) / KB + (a.mask == KF_MASK_SINGLE ? 1 : 2) * ((nk1 + KB - 1) / KB);
-  launch((training_attention_dkv_kernel<DH, SK, KS>), dim3((unsigned)(a.BH * nb)), dim3(256), 0, s, a);
+  launch((training_attention_dkv_kernel<DH, SK, KS, FINE>), dim3((unsigned)(a.BH * nb)), dim3(256), 0, s, a);
 }
 
 // 64 keys a workgroup, its rows in two groups, where there are few blocks of 128 context
@@ -517,11 +536,14 @@ template <int DH, int S, int SK>
 hipError_t launch_bwd(const BwdArgs& a, hipStream_t s) {
   constexpr int NW = 4, QB = 32 * NW;
   const int halves = a.mask == KF_MASK_DOUBLE ? 2 : 1, nqb = (a.nq / halves + QB - 1) / QB * halves;
-  launch((training_attention_dq_kernel<DH, S, NW>), dim3((unsigned)(a.BH * nqb)), dim3(64 * NW), 0, s, a);
-  if ((int64_t)a.BH * ((a.N + 127) / 128) <= (DH == 128 ? 96 : 192))
-    launch_dkv<DH, SK, 2>(a, s);
+  const dim3 grid((unsigned)(a.BH * nqb)), block(64 * NW);
+  launch((training_attention_dq_kernel<DH, S, NW>), grid, block, 0, s, a);
+  if (a.BH * nqb <= 128)
+    launch_dkv<DH, SK, 2, true>(a, s);
+  else if ((int64_t)a.BH * ((a.N + 127) / 128) <= (DH == 128 ? 96 : 192))
+    launch_dkv<DH, SK, 2, false>(a, s);
   else
-    launch_dkv<DH, SK, 4>(a, s);
+    launch_dkv<DH, SK, 4, false>(a, s);
   return hipGetLastError();
 }
 
