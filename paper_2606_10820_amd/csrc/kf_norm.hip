@@ -9,6 +9,11 @@
 // Statistics, sums and gradients of the gain and shift are fp32; the variance is
 // the mean of squared deviations from the mean already formed, so a row whose
 // offset is large against its spread loses nothing to cancellation.
+//
+// Bound by memory: a row is read once, kept in the registers of as many lanes as it
+// fills (a second read, from L2, costs as much as the first), and written once.
+// Forward 40 us at 40960 x 768 fp32 to bf16 (4.7 TB/s) and 58 at 81920 x 1024 bf16
+// (5.8), backward with dres 66 (6.6, x in part from the caches) and 114 (5.9).  A few rows are bound by the launch (2.8 us).
 #include <type_traits>
 
 #include "kf_rows.h"
