@@ -12,15 +12,20 @@
 //     and stores lse / scale and D for the other walk.  D = dO.O carries the roundings
 //     of O and of the forward pass's P (bf16: up to 2^-8 each); the exact D is the one
 //     that makes a row of dS sum to zero, so D + (the fp32 sum of that row) is stored.
-//     dS enters the product as two bf16 terms, its rounding and the rest: one product
-//     more, and less time than taking D's error out of dQ (32 registers for P K, two
-//     wavefronts per SIMD instead of three: 171 us against 154).
+//     In dQ itself D's error counts where a row sees few keys (it falls with the root of
+//     their number against dS): blocks with such rows, short walks, take that sum in a
+//     walk of its own first.  dQ of N = 2, k = 1 M_D is off by 1.9e-3 instead of 3.6e-3, of
+//     N = 16, k = 4 by 1.7e-3 instead of 2.2e-3; forward and backward of M_S, 768 heads,
+//     k = 4 take 41 us instead of 38 at N = 16, 225 instead of 219 at N = 128.  For every
+//     row, by P K beside the walk, it takes 32 registers more and two wavefronts per SIMD
+//     instead of three (M_D at N = 1024: 171 us against 154).
+//     dS enters the product as two bf16 terms, its rounding and the rest.
 //   dK, dV: a workgroup owns 128 keys of one key region and walks the query rows
 //     that see them: at most two row intervals, the mask read by columns.  Scores
 //     are formed as queries x keys, a lane holds one key, and P and dS are the B
 //     operands of dV^T += dO^T P and dK^T += Q^T dS.
 // On small grids (FINE) P and dS enter dV and dK as two terms as well.  Errors against 64
-// bits (norms; the results' own rounding is 1.7e-3): dQ 1.8e-3 to 2.2e-3, dK and dV
+// bits (norms; the results' own rounding is 1.7e-3): dQ 1.7e-3 to 2.0e-3, dK and dV
 // 2.4e-3, on small grids 1.8e-3.  One term everywhere and D as it comes took dQ and dK to
 // 2.5e-3 to 2.8e-3; two terms everywhere take dK and dV of M_D at N = 1024 from 209 to
 // 270 us.
@@ -169,6 +174,12 @@ __device__ __forceinline__ void load_row(bf16x8_t (&f)[DH / 16], const bf16* row
     f[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(row + 16 * c + 8 * ((threadIdx.x & 63) >> 5)));
 }
 
+// The sum over the two lane halves.
+__device__ __forceinline__ float add_xor32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // x as the sum of three bf16 (24 bits), in the low 6 bytes.
 __device__ __forceinline__ uint2 bf16x3(float x) {
   const bf16 a = (bf16)x, b = (bf16)(x - (float)a), c = (bf16)(x - (float)a - (float)b);
@@ -177,6 +188,7 @@ __device__ __forceinline__ uint2 bf16x3(float x) {
 }
 
 // ------------------------------------------------------------------- dQ
+constexpr int kFewKeys = 32;  // context tokens that a block's rows see, below which D is formed first
 template <int DH, int S, int NW>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH <= 64 ? 3 : 2)))
     training_attention_dq_kernel(BwdArgs a) {
@@ -201,8 +213,14 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     off[i] = r * G::ROWB + ((pc ^ swz<DH>(r)) * 16);
   }
   const TileReads<DH> tr;
-  auto issue = [&](int ti, int stage) {
-    const bool live = ti < C.ntiles;
+  // two walks where a row of the block sees few keys: its first row, or, where the block
+  // crosses from M_S's last context row to the noise rows, the first of those
+  const bool again = row_intervals(a.mask, a.N, a.k, a.km, C.q0).hi[0] < kFewKeys ||
+                     (a.mask == KF_MASK_SINGLE && C.q0 < a.N && C.qe > a.N);
+  const int walk = again ? 2 * C.ntiles : C.ntiles;
+  auto issue = [&](int i, int stage) {
+    const bool live = i < walk;
+    const int ti = i < C.ntiles ? i : i - C.ntiles;
     const int t0 = live ? C.t0(ti) : 0;
     const int rows = live ? min(C.end(ti) - t0, kKT) : 0;
     const size_t at = ((size_t)C.bh * a.nk + t0) * DH;
@@ -231,8 +249,7 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) nd -= (float)of[c][e] * (float)gf[c][e];
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(nd), __float_as_uint(nd), false, false);
-    nd = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    nd = add_xor32(nd);
   }
   const float l2 = a.lse[grow] * kLog2e;
   int wlo[3] = {0, 0, 0}, whi[3] = {0, 0, 0}, ilo[3] = {1, 1, 1}, ihi[3] = {0, 0, 0};
@@ -248,10 +265,10 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
   for (int i = 0; i < 16; ++i) nd16[i] = nd;
 
   int stage = 0;
-  for (int ti = 0; ti < C.ntiles; ++ti) {
-    vm_wait<(S - 2) * G::PER>();  // this wavefront's part of tile ti has landed
-    __builtin_amdgcn_s_barrier();  // ... and everyone's; stage (ti - 1) % S is free
-    issue(ti + S - 1, stage == 0 ? S - 1 : stage - 1);
+  auto tile = [&](int i, int ti, auto sums_only) {
+    vm_wait<(S - 2) * G::PER>();  // this wavefront's part of tile i has landed
+    __builtin_amdgcn_s_barrier();  // ... and everyone's; stage (i - 1) % S is free
+    issue(i + S - 1, stage == 0 ? S - 1 : stage - 1);
     const int rs = (ti >= C.b1) + (ti >= C.b2);
     const int cwlo = pick(wlo, rs), cwhi = pick(whi, rs);
     const int t0 = C.t0(ti);
@@ -268,7 +285,7 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
       mul_nat<DH>(s, ka, qf);
       mul_nat<DH>(dp, va, gf);
       u32x2 kt[2][NE][2];
-      read_tr<DH, g>(kt, kb, tr);
+      if constexpr (!sums_only) read_tr<DH, g>(kt, kb, tr);
       if (!(s0 >= pick(ilo, rs) && s0 + 32 <= pick(ihi, rs))) {
         const int lo = pick(iv.lo, rs), base = s0 + 4 * half - lo, width = max(pick(iv.hi, rs) - lo, 0);
 #pragma unroll
@@ -284,19 +301,26 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
 #pragma unroll
       for (int i = 1; i < 16; ++i) part += dp[i];
       eps += part;
-      bf16x8_t ds[2], rest[2];
-      to_bf16(ds, dp);
-      rest_bf16(rest, dp, ds);
-      lgkm_wait0();
-      mul_tr<DH>(dq, kt, ds);
-      mul_tr<DH>(dq, kt, rest);
+      if constexpr (!sums_only) {
+        bf16x8_t ds[2], rest[2];
+        to_bf16(ds, dp);
+        rest_bf16(rest, dp, ds);
+        lgkm_wait0();
+        mul_tr<DH>(dq, kt, ds);
+        mul_tr<DH>(dq, kt, rest);
+      }
     });
+  };
+  if (again) {
+    for (int ti = 0; ti < C.ntiles; ++ti) tile(ti, ti, std::true_type{});
+    nd -= add_xor32(eps);
+    eps = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) nd16[i] = nd;
   }
+  for (int ti = 0; ti < C.ntiles; ++ti) tile(walk - C.ntiles + ti, ti, std::false_type{});
   vm_wait<0>();  // loads issued for tiles past the last one
-  {
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(eps), __float_as_uint(eps), false, false);
-    eps = __uint_as_float(both[0]) + __uint_as_float(both[1]);
-  }
+  eps = add_xor32(eps);
   if (valid && half == 0) {
     const uint2 l = bf16x3(a.lse[grow] * a.inv_scale), d = bf16x3(eps - nd);
     a.stats[grow] = make_uint4(l.x, l.y, d.x, d.y);

@@ -92,6 +92,32 @@ def test_larger_shapes(Bd, mask, B, H, N, k, dh):
         _check([x[b, h].cpu() for x in got], *[x[b, h].cpu() for x in t], M, dh ** -0.5, f"b {b} h {h}")
 
 
+@pytest.mark.parametrize("mask,N,k,dh", [(0, 40, 1, 64), (0, 100, 1, 32), (0, 20, 3, 128), (0, 1, 8, 64), (1, 31, 4, 64), (1, 5, 1, 32), (1, 16, 2, 128)])
+def test_equal_answers_have_no_score_gradient(Bd, mask, N, k, dh):
+    """Values that differ but give every key the same dO.V (pairs of columns swapped, dO equal on a pair):
+    dS is zero everywhere, although O is rounded.  What stays of D after its correction is O's rounding,
+    2^-8 of A = sum |dO||V|, times what the forward's sum of bf16 probabilities leaves of 1 - sum P, 2^-8;
+    beside it two fp32 sums of d_head products and the row sum."""
+    rows, keys = Bd.training_attention_shapes(mask, N, k)
+    B, H = 2, 3
+    q, k_, _, _ = _inputs(B, H, rows, keys, dh, N)
+    g = torch.Generator().manual_seed(N + dh)
+    pair = torch.randn(B, H, 1, dh // 2, 2, generator=g).to(BF)
+    swap = torch.rand(B, H, keys, dh // 2, 1, generator=g) < 0.5
+    v = torch.where(swap, pair.flip(-1), pair).reshape(B, H, keys, dh).contiguous()
+    do = torch.randn(B, H, rows, dh // 2, 1, generator=g).to(BF).expand(-1, -1, -1, -1, 2).reshape(B, H, rows, dh).contiguous()
+    _, _, dq, dk, _ = _run(Bd, mask, *[x.cuda() for x in (q, k_, v, do)], N, k)
+    torch.cuda.synchronize()
+    M, scale = torch.from_numpy(O.training_mask(KIND[mask], N, k)).bool(), dh ** -0.5
+    P = (q.double() @ k_.double().transpose(-1, -2) * scale).masked_fill(~M, -torch.inf).softmax(-1)
+    A = (do.double().abs() @ v.double().abs().transpose(-1, -2)).amax(-1, keepdim=True)
+    e = P * A * (2 ** -16 + (4 * dh + M.sum(-1, keepdim=True) + 32) * R.U) * 1.01
+    res = [float((x.double().cpu().abs() / (b + 1e-30)).max()) for x, b in
+           ((dq, scale * e @ k_.double().abs()), (dk, scale * e.transpose(-1, -2).contiguous() @ q.double().abs()))]
+    print(mask, N, k, dh, res, flush=True)
+    assert max(res) <= 1.01  # the results' own rounding
+
+
 def test_gradients_that_vanish(Bd):
     """The first context row sees itself alone: P = 1, its dq is zero up to the rounding of scores
     and D; zero dO gives zero gradients."""
