@@ -34,11 +34,11 @@
 // Operands that a product needs with the other index first come through the
 // transposing LDS reads of the same tiles.
 //
-// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 152 us, dK and dV 208 (361 TFLOP/s of the
+// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 159 us, dK and dV 211 (352 TFLOP/s of the
 // 5 products of the visible pairs).  Neither bytes nor matrix rate bound it but latency:
 // a wavefront's chain from LDS through two products, the exponential and two more, with
 // the 3 (dQ) and 2 (dK, dV) wavefronts a SIMD that the registers allow.  M_S, 768 heads,
-// N = 128: 79 and 89 us for 386 MB each (Q, K, V, dO are read by both walks), 4.9 and 4.3
+// N = 128: 86 and 88 us for 385 MB each (Q, K, V, dO are read by both walks), 4.5 and 4.4
 // TB/s: memory bounds it.
 #include "kf_blockattn.h"
 #include "kf_train.h"
