@@ -21,6 +21,11 @@ namespace kf {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// exp2 of this and of anything below is zero.  Differences from the maximum (log2 units,
+// minus infinity for a masked logit) are raised to it where they are a factor beside that
+// exponential: the product is then zero whatever the entropy's weight (a factor of size 3e38
+// overflowed from weights of 1.64 on, and zero times infinity is NaN).
+constexpr float kNoShare = -256.f;
 
 // Order of the alternatives: larger logits first, equal ones by the lower id; NaN
 // before everything, and -0 equal to 0.
@@ -209,7 +214,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
     auto sum = [&](float v) {
       const float t = (v - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
       s += e;
-      w = __builtin_fmaf(e, fmaxf(t, -3e38f), w);
+      w = __builtin_fmaf(e, fmaxf(t, kNoShare), w);
     };
     // (m, s, w) against the larger maximum `to`
     auto rebase = [&](float from, float to) {
@@ -291,8 +296,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
       const float k0 = empty ? 0.f : -(u + c * (H - ls)) * inv, k1 = -c * kLn2 * inv;
       auto grad = [&](float v) {
         const float t = (v - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
-        // c = 0 leaves k1 zero, which a term of minus infinity would turn into NaN
-        return e * __builtin_fmaf(k1, fmaxf(t, -3e38f), k0);
+        return e * __builtin_fmaf(k1, fmaxf(t, kNoShare), k0);
       };
       const bool same = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(x)) & 15) == 0;
       const int tv = tok >= head && tok < tail0 ? (tok - head) / E : -1;  // the token's vector
