@@ -672,7 +672,8 @@ class GradClip:
     kf_grad_clip): a plan over the tensors `grads`, which it keeps.
 
     out: where the scaled gradients go, a tensor for each (of its type or fp32); default the
-    gradients themselves.  The plan is built on `stream` and used on one stream at a time."""
+    gradients themselves.  The plan is built on `stream` and used on one stream at a time; it
+    may be dropped while calls still run, but not while a graph that captured one is in use."""
 
     def __init__(self, grads, out=None, stream=None):
         import torch
@@ -694,6 +695,7 @@ class GradClip:
             raise KfError(KF_EINVAL, "kf_grad_plan_bytes rejected the tensors")
         self.plan = KfGradPlan()
         s, ctx = _on(self.device, stream, ())
+        self.stream = s  # whose memory buf is
         with ctx:
             self.buf = torch.empty(n + 256, dtype=torch.uint8, device=self.device)
             _ok(lib().kf_grad_plan_init(s, len(self.grads), arr,
@@ -702,7 +704,9 @@ class GradClip:
 
     def _call(self, stream, f, *more):
         import torch
-        s, ctx = _on(self.device, stream, (self.buf, *self.grads, *self.out) if stream else ())
+        s, ctx = _on(self.device, stream, (*self.grads, *self.out) if stream else ())
+        if s != self.stream:  # buf may go back to its own stream while this one still reads it
+            self.buf.record_stream(stream or torch.cuda.current_stream(self.device))
         with ctx:
             norm = torch.empty((), dtype=torch.float32, device=self.device)
             _ok(f(s, self.plan, *more, norm.data_ptr()))
