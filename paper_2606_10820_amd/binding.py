@@ -443,6 +443,8 @@ def _on(device, stream, used):
     global _current_raw, _current_device
     if device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
+    if stream is not None and stream.device != device:  # (every device's default stream has handle 0)
+        raise ValueError("the stream is another device's")
     import torch
     if _current_device is None:
         _current_device = torch.cuda.current_device
@@ -451,8 +453,6 @@ def _on(device, stream, used):
             lambda i: torch.cuda.current_stream(i).cuda_stream)
     raw = _current_raw(device.index)
     if stream is not None and stream.cuda_stream != raw:
-        if stream.device != device:
-            raise ValueError("the stream is another device's")
         for t in used:
             if t is not None:
                 t.record_stream(stream)
