@@ -482,9 +482,10 @@ int kf_grad_norm(void *hip_stream, const kf_grad_plan *plan, float *norm);
 
 /* dst = src * (norm > max_norm ? max_norm / norm : 1) for every tensor, and the
  * norm before clipping into norm (device; may be null).  max_norm >= 0
- * (infinity: never clip).  A norm that is not finite (infinities or NaN among
- * the gradients) scales nothing: the caller sees it in norm.  KF_EINVAL for a
- * plan with a tensor without a dst. */
+ * (infinity: never clip).  A norm that is not finite in fp32 (infinities or NaN
+ * among the gradients, or finite ones whose norm is past 3.4e38) scales nothing:
+ * the caller sees it in norm.  KF_EINVAL for a plan with a tensor without a
+ * dst. */
 int kf_grad_clip(void *hip_stream, const kf_grad_plan *plan, float max_norm, float *norm);
 
 /* ----------------------------------------------------- continuous batching

@@ -133,8 +133,8 @@ __global__ void __launch_bounds__(256)
   __shared__ double red[4];
   const double v = join_norm(part, n_part, red);
   if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = (float)v;
-  // a norm that is not finite scales nothing
-  const float f = v > (double)max_norm && v < (double)INFINITY ? (float)((double)max_norm / v) : 1.0f;
+  // a norm that is not finite as it is returned, in fp32, scales nothing
+  const float f = v > (double)max_norm && (float)v < INFINITY ? (float)((double)max_norm / v) : 1.0f;
   // last chunks first: they are the ones that the caches still hold
   for (int64_t i = chunks - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
     const GradChunk c = table[i];
