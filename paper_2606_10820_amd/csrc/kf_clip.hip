@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(256)
 // vectors of the wider type (130 M gradients, bf16 into fp32: 234 -> 165 us; fp32 301 ->
 // 250).
 template <typename S, typename D>
-__device__ void chunk_scale(const GradChunk& c, float f) {
+__device__ void chunk_scale(const GradChunk& c, float f, float f2) {
   const S* x = static_cast<const S*>(c.src);
   D* y = static_cast<D*>(c.dst);
   auto scale = [&](auto e, int i) {
@@ -118,7 +118,7 @@ __device__ void chunk_scale(const GradChunk& c, float f) {
     float t[E];
     stream_in<E>(x + i, t);
 #pragma unroll
-    for (int j = 0; j < E; ++j) t[j] *= f;
+    for (int j = 0; j < E; ++j) t[j] = t[j] * f * f2;
     stream_out<E>(y + i, t);
   };
   constexpr int VE = 16 / (sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D));
@@ -134,17 +134,21 @@ __global__ void __launch_bounds__(256)
   const double v = join_norm(part, n_part, red);
   if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = (float)v;
   // a norm that is not finite as it is returned, in fp32, scales nothing
-  const float f = v > (double)max_norm && (float)v < INFINITY ? (float)((double)max_norm / v) : 1.0f;
+  const double r = v > (double)max_norm && (float)v < INFINITY ? (double)max_norm / v : 1.0;
+  // r = f f2.  Below fp32's normal numbers r would lose bits, or all of them: f is then r 2^120,
+  // which keeps a product below 2^122 (max_norm is at most 4 there), and f2 undoes that.
+  const bool tiny = r < 0x1p-126;
+  const float f = (float)(tiny ? r * 0x1p120 : r), f2 = tiny ? 0x1p-120f : 1.0f;
   // last chunks first: they are the ones that the caches still hold
   for (int64_t i = chunks - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
     const GradChunk c = table[i];
     if (f == 1.0f && c.dst == c.src) continue;  // in place and unscaled: there already
     switch (c.types) {
-      case KF_FP32 + 4 * KF_FP32: chunk_scale<float, float>(c, f); break;
-      case KF_BF16 + 4 * KF_BF16: chunk_scale<bf16, bf16>(c, f); break;
-      case KF_FP16 + 4 * KF_FP16: chunk_scale<f16, f16>(c, f); break;
-      case KF_BF16 + 4 * KF_FP32: chunk_scale<bf16, float>(c, f); break;
-      default: chunk_scale<f16, float>(c, f); break;
+      case KF_FP32 + 4 * KF_FP32: chunk_scale<float, float>(c, f, f2); break;
+      case KF_BF16 + 4 * KF_BF16: chunk_scale<bf16, bf16>(c, f, f2); break;
+      case KF_FP16 + 4 * KF_FP16: chunk_scale<f16, f16>(c, f, f2); break;
+      case KF_BF16 + 4 * KF_FP32: chunk_scale<bf16, float>(c, f, f2); break;
+      default: chunk_scale<f16, float>(c, f, f2); break;
     }
   }
 }
