@@ -298,27 +298,32 @@ __global__ void __launch_bounds__(256) norm_cols_any_kernel(NormGradArgs a, int 
   p[a.d + c] = b;
 }
 
-// The strips' sums joined: 32 columns of [dg | db] by 32 groups of strips a
-// workgroup.  Also writes the zeros of an empty batch (strips 0).
+// The strips' sums joined: 32 columns of [dg | db] by 32 groups of strips at a time, a
+// workgroup over every gridDim-th of them (wide rows have more than a launch has
+// workgroups of 1024).  Also writes the zeros of an empty batch (strips 0).
 __global__ void __launch_bounds__(1024) norm_cols_join_kernel(const float* __restrict__ part,
                                                               int strips, int d, float* dgain,
                                                               float* dshift) {
   __shared__ float sum[32][33];
-  const int c = threadIdx.x & 31, grp = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
-  float v = 0.f;
-  if (col < 2 * d) {
+  const int c = threadIdx.x & 31, grp = threadIdx.x >> 5;
+  for (int col0 = blockIdx.x * 32; col0 < 2 * d; col0 += gridDim.x * 32) {
+    const int col = col0 + c;
+    float v = 0.f;
+    if (col < 2 * d) {
 #pragma unroll 8
-    for (int s = grp; s < strips; s += 32) v += part[(size_t)s * 2 * d + col];
-  }
-  sum[grp][c] = v;
-  __syncthreads();
-  if (grp || col >= 2 * d) return;
+      for (int s = grp; s < strips; s += 32) v += part[(size_t)s * 2 * d + col];
+    }
+    if (col0 != (int)blockIdx.x * 32) __syncthreads();  // the columns before have been read
+    sum[grp][c] = v;
+    __syncthreads();
+    if (grp || col >= 2 * d) continue;
 #pragma unroll
-  for (int i = 1; i < 32; ++i) v += sum[i][c];
-  if (col < d) {
-    if (dgain) dgain[col] = v;
-  } else if (dshift) {
-    dshift[col - d] = v;
+    for (int i = 1; i < 32; ++i) v += sum[i][c];
+    if (col < d) {
+      if (dgain) dgain[col] = v;
+    } else if (dshift) {
+      dshift[col - d] = v;
+    }
   }
 }
 
@@ -428,9 +433,11 @@ hipError_t launch_norm_grad(const NormGradArgs& args, hipStream_t s) {
       const hipError_t e = vec ? by_width<VE>(a.d, rows, any) : by_width<1>(a.d, rows, any);
       if (e != hipSuccess) return e;
     }
-    if (sums)
-      launch(norm_cols_join_kernel, dim3((unsigned)((2 * (int64_t)a.d + 31) / 32)), dim3(1024), 0, s,
-             a.part, strips, a.d, a.dgain, a.dshift);
+    if (sums) {
+      const int blocks = (2 * a.d + 31) / 32;
+      launch(norm_cols_join_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(1024), 0,
+             s, a.part, strips, a.d, a.dgain, a.dshift);
+    }
     return hipGetLastError();
   });
 }
