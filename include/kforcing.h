@@ -327,8 +327,9 @@ int kf_kernel_time(kf_ctx *ctx, int kernel_class, double *total_ms, int *launche
  *   launched, pointers unchecked).
  * Returns KF_EINVAL for an unknown mask, k < 1, a negative size, an unsupported
  * d_head, a non-finite scale, a null or misaligned pointer, or a problem whose
- * per-head element count or workgroup count reaches 2^31; KF_EHIP when the
- * launch fails.  There is no context, hence no kf_last_error() message. */
+ * per-head element count reaches 2^31 or whose workgroups (of 64 or 128 query
+ * rows of a head) reach 2^24, the threads of a launch; KF_EHIP when the launch
+ * fails.  There is no context, hence no kf_last_error() message. */
 #define KF_MASK_SINGLE 0
 #define KF_MASK_DOUBLE 1
 int kf_training_attention(void *hip_stream, int mask, int B, int H, int N, int k, int d_head,
@@ -352,7 +353,9 @@ int kf_training_attention_lse(void *hip_stream, int mask, int B, int H, int N, i
  * dS for dV and dK likewise where there are few rows), all sums are fp32 and of a
  * fixed order (no atomics: a call's result is the same on every run).
  * Inputs are finite: an infinity or NaN may spread to rows and keys of its head
- * that do not see it.  scale in [1e-20, 1e20], keys * k below 2^32.
+ * that do not see it.  scale in [1e-20, 1e20], keys * k below 2^32, blocks of
+ * 128 keys (the context's and each noise region's by themselves) of all heads
+ * below 2^24; kf_training_attention_lse refuses what this call would.
  * workspace: kf_training_attention_backward_bytes() bytes of device memory,
  * 16-byte aligned, used during the call only; calls that overlap need one
  * each.  The size is 0 for arguments that the call refuses and for an empty

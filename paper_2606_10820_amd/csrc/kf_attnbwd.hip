@@ -41,6 +41,7 @@
 // N = 128: 86 and 88 us for 385 MB each (Q, K, V, dO are read by both walks), 4.5 and 4.4
 // TB/s: memory bounds it.
 #include "kf_blockattn.h"
+#include "kf_route.h"
 #include "kf_train.h"
 
 namespace kf {
@@ -552,26 +553,18 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 
 
 template <int DH, int SK, int KS, bool FINE>
 void launch_dkv(const BwdArgs& a, hipStream_t s) {
-  constexpr int KB = 32 * KS;
-  const int nk1 = a.N * a.k;
-  const int nb = (a.N + KB - 1) / KB + (a.mask == KF_MASK_SINGLE ? 1 : 2) * ((nk1 + KB - 1) / KB);
+  const int nb = (int)backward_key_blocks(a.mask == KF_MASK_DOUBLE, a.N, a.k, 32 * KS);
   launch((training_attention_dkv_kernel<DH, SK, KS, FINE>), dim3((unsigned)(a.BH * nb)), dim3(256), 0, s, a);
 }
 
-// 64 keys a workgroup, its rows in two groups, where there are few blocks of 128 context
-// keys (the long ones); 128 keys otherwise.  us of both walks, 64 | 128 keys, by the
-// number of those blocks: d_head 64 48 57 | 68, 96 154 | 186, 192 81 | 88 and 181 | 215,
-// 288 240 | 244, 384 313 | 283; d_head 32 96 26 | 30, 192 40 | 39; d_head 128 96 87 | 99,
-// 192 161 | 130.
 template <int DH, int S, int SK>
 hipError_t launch_bwd(const BwdArgs& a, hipStream_t s) {
-  constexpr int NW = 4, QB = 32 * NW;
-  const int halves = a.mask == KF_MASK_DOUBLE ? 2 : 1, nqb = (a.nq / halves + QB - 1) / QB * halves;
-  const dim3 grid((unsigned)(a.BH * nqb)), block(64 * NW);
-  launch((training_attention_dq_kernel<DH, S, NW>), grid, block, 0, s, a);
+  constexpr int NW = 4;
+  const int nqb = (int)backward_row_blocks(a.mask == KF_MASK_DOUBLE, a.N, a.k);
+  launch((training_attention_dq_kernel<DH, S, NW>), dim3((unsigned)(a.BH * nqb)), dim3(64 * NW), 0, s, a);
   if (a.BH * nqb <= 128)
     launch_dkv<DH, SK, 2, true>(a, s);
-  else if ((int64_t)a.BH * ((a.N + 127) / 128) <= (DH == 128 ? 96 : 192))
+  else if (backward_keys(DH, a.BH, a.N) == 64)
     launch_dkv<DH, SK, 2, false>(a, s);
   else
     launch_dkv<DH, SK, 4, false>(a, s);

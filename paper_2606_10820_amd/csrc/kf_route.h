@@ -58,6 +58,39 @@ inline TrainingRoute training_route(int dh, long long BH, bool two_parts, long l
   return {r32, (int)prow, (int)b32};
 }
 
+// Workgroups of a training attention call, 256 threads each.
+inline long long training_groups(int dh, long long BH, bool two_parts, long long N, long long k) {
+  const long long nq = two_parts ? 2 * N * k : N + N * k;
+  const TrainingRoute r = training_route(dh, BH, two_parts, N, k, nq);
+  return BH * (r.rows32 ? r.blocks32 : (nq + 63) / 64);
+}
+
+// Its gradients: workgroups of the dQ walk, 128 query rows each (M_D's halves by
+// themselves), and keys of a workgroup of the dK, dV walk.  64, its rows in two groups,
+// where there are few blocks of 128 context keys (the long ones); 128 otherwise.  us of
+// both walks, 64 | 128 keys, by the number of those blocks: d_head 64 48 57 | 68, 96
+// 154 | 186, 192 81 | 88 and 181 | 215, 288 240 | 244, 384 313 | 283; d_head 32 96
+// 26 | 30, 192 40 | 39; d_head 128 96 87 | 99, 192 161 | 130.
+inline long long backward_row_blocks(bool two_parts, long long N, long long k) {
+  return two_parts ? 2 * ((N * k + 127) / 128) : (N + N * k + 127) / 128;
+}
+inline int backward_keys(int dh, long long BH, long long N) {
+  return BH * ((N + 127) / 128) <= (dh == 128 ? 96 : 192) ? 64 : 128;
+}
+inline long long backward_key_blocks(bool two_parts, long long N, long long k, int keys) {
+  return (N + keys - 1) / keys + (two_parts ? 2 : 1) * ((N * k + keys - 1) / keys);
+}
+// The larger walk's.
+inline long long backward_groups(int dh, long long BH, bool two_parts, long long N, long long k) {
+  const long long q = backward_row_blocks(two_parts, N, k),
+                  kv = backward_key_blocks(two_parts, N, k, backward_keys(dh, BH, N));
+  return BH * (q > kv ? q : kv);
+}
+
+// Workgroups of 256 threads that one launch holds: its threads are counted in 32 bits,
+// and those past them are dropped without an error.
+constexpr long long kMaxGroups256 = (1LL << 24) - 1;
+
 // Block attention of a step over the paged KV cache (bf16).  Three kernels:
 //   split  one workgroup of four wavefronts (two for contexts of at most 128 keys)
 //          per 16 query rows and key split, ns splits, and a merge kernel if ns > 1

@@ -4,6 +4,7 @@
 #include <stdlib.h>
 
 #include "kforcing.h"
+#include "kf_route.h"
 #include "kf_train.h"
 
 namespace {
@@ -91,6 +92,8 @@ int kf::check_training_attention(int mask, int B, int H, int N, int k, int d_hea
   const int64_t lim = (int64_t)1 << 31;
   if (keys * d_head >= lim || (int64_t)B * H >= lim || (int64_t)B * H * ((rows + 63) / 64) >= lim)
     return KF_EINVAL;
+  if (training_groups(d_head, (int64_t)B * H, mask == KF_MASK_DOUBLE, N, k) > kMaxGroups256)
+    return KF_EINVAL;
   return KF_OK;
 }
 
@@ -98,10 +101,11 @@ namespace {
 // The limits of the calls with gradients: q / k by a reciprocal, workgroups of both
 // walks; a scale of zero or less turns a masked score, minus infinity, into NaN or a
 // maximum, and lse / scale is stored.
-bool attn_grad_fits(int mask, int B, int H, int N, int k, float scale) {
+bool attn_grad_fits(int mask, int B, int H, int N, int k, int d_head, float scale) {
   if (!(scale >= 1e-20f && scale <= 1e20f)) return false;
   const int64_t nk = (int64_t)N * k, keys = mask == KF_MASK_SINGLE ? N + nk : N + 2 * nk;
-  return keys * k < ((int64_t)1 << 32) && (int64_t)B * H * (keys / 32 + 4) < ((int64_t)1 << 31);
+  return keys * k < ((int64_t)1 << 32) &&
+         kf::backward_groups(d_head, (int64_t)B * H, mask == KF_MASK_DOUBLE, N, k) <= kf::kMaxGroups256;
 }
 }  // namespace
 
@@ -113,7 +117,7 @@ int kf_training_attention_lse(void* hip_stream, int mask, int B, int H, int N, i
   const void* ptrs[5] = {Q, K, V, O, lse};
   const int rc = kf::check_training_attention(mask, B, H, N, k, d_head, scale, ptrs, 5);
   if (rc) return rc < 0 ? rc : KF_OK;
-  if (!attn_grad_fits(mask, B, H, N, k, scale)) return KF_EINVAL;
+  if (!attn_grad_fits(mask, B, H, N, k, d_head, scale)) return KF_EINVAL;
   return code(kf::launch_training_attention(mask, B, H, N, k, d_head, static_cast<const bf16*>(Q),
                                             static_cast<const bf16*>(K),
                                             static_cast<const bf16*>(V), static_cast<bf16*>(O),
@@ -122,7 +126,7 @@ int kf_training_attention_lse(void* hip_stream, int mask, int B, int H, int N, i
 
 size_t kf_training_attention_backward_bytes(int mask, int B, int H, int N, int k, int d_head) {
   if (kf::check_training_attention(mask, B, H, N, k, d_head, 1.0f, nullptr, 0) != KF_OK ||
-      !attn_grad_fits(mask, B, H, N, k, 1.0f))
+      !attn_grad_fits(mask, B, H, N, k, d_head, 1.0f))
     return 0;
   return kf::training_attention_backward_bytes(mask, B, H, N, k);
 }
@@ -135,7 +139,7 @@ int kf_training_attention_backward(void* hip_stream, int mask, int B, int H, int
   const void* ptrs[10] = {Q, K, V, O, lse, dO, dQ, dK, dV, workspace};
   const int rc = kf::check_training_attention(mask, B, H, N, k, d_head, scale, ptrs, 10);
   if (rc) return rc < 0 ? rc : KF_OK;
-  if (!attn_grad_fits(mask, B, H, N, k, scale) ||
+  if (!attn_grad_fits(mask, B, H, N, k, d_head, scale) ||
       workspace_bytes < kf::training_attention_backward_bytes(mask, B, H, N, k))
     return KF_EINVAL;
   return code(kf::launch_training_attention_backward(
