@@ -175,12 +175,6 @@ __device__ __forceinline__ void load_row(bf16x8_t (&f)[DH / 16], const bf16* row
     f[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const uint4*>(row + 16 * c + 8 * ((threadIdx.x & 63) >> 5)));
 }
 
-// The sum over the two lane halves.
-__device__ __forceinline__ float add_xor32(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 // x as the sum of three bf16 (24 bits), in the low 6 bytes.
 __device__ __forceinline__ uint2 bf16x3(float x) {
   const bf16 a = (bf16)x, b = (bf16)(x - (float)a), c = (bf16)(x - (float)a - (float)b);

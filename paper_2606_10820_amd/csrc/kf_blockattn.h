@@ -132,6 +132,12 @@ __device__ inline float max_xor32(float x) {
   return max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// The sum over the two lane halves.
+__device__ inline float add_xor32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Tile geometry.  A stage holds the K tile then the V tile.  K, and V of a
 // training call, are [64 keys][DH] bf16 in natural layout with 16-byte chunks
 // permuted within each row: logical chunk c of key row r sits at chunk

@@ -75,6 +75,12 @@ struct RowSets {
   int glo, ghi;        // keys inside a union that no row of the wavefront sees
 };
 
+// The log of a row's sum of exponentials (natural), from its reference m in log2
+// units and its sum over exp2(score - m).
+__device__ __forceinline__ float row_lse(float m, float sum) {
+  return (m + log2f(sum)) * 0.6931471805599453f;
+}
+
 // One work item: the unnormalised O^T and row sum of this lane's query row
 // (row lane & 31 of its wavefront's 32), lane half h = lane >> 5 holding d_head
 // indices 32 eg + 8 (i / 4) + 4 h + i % 4 of o[eg][i].
@@ -89,10 +95,14 @@ struct RowSets {
 // Scores of the next tile formed under the softmax of this one (two score
 // blocks, 239 registers, two wavefronts per SIMD instead of three) took 342 us;
 // four wavefronts per SIMD spill (324 us); a third stage changes nothing.
-template <int DH, int S, int NW, class Keys>
+//
+// LSE: lx is the row's log sum of exponentials.  Its terms are the fp32 probabilities, not
+// the rounded ones whose sum o is divided by: those put it off by up to 2^-9 where a row sees
+// few keys, and with it every probability of the backward pass.
+template <int DH, int S, int NW, bool LSE = false, class Keys>
 __device__ __forceinline__ void attend(unsigned char* smem, const Item& C, const Keys& keys,
                                        const RowSets& rs_, const bf16x8_t (&qf)[DH / 16], float c2,
-                                       f32x16_t (&o)[DH / 32], float& ls, float& m_run) {
+                                       f32x16_t (&o)[DH / 32], float& ls, float& lx) {
   using G = Geo<DH, S, NW>;
   constexpr int NC = DH / 16, NE = DH / 32;
   const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -151,8 +161,8 @@ __device__ __forceinline__ void attend(unsigned char* smem, const Item& C, const
   // running max m (log2 units); o = the unnormalised O^T; ls = this lane's part
   // of the row sum: over the bf16 probabilities that o uses, or, in a model's step
   // over the cache, over the fp32 ones as in the other kernels of block attention
-  m_run = -INFINITY;
-  ls = 0.f;
+  float m_run = -INFINITY;
+  ls = lx = 0.f;
 #pragma unroll
   for (int eg = 0; eg < NE; ++eg)
 #pragma unroll
@@ -233,6 +243,7 @@ __device__ __forceinline__ void attend(unsigned char* smem, const Item& C, const
       const float mn = grow ? mx : m_run;
       const float alpha = __builtin_amdgcn_exp2f(m_run - mn);
       ls *= alpha;
+      if (LSE) lx *= alpha;
 #pragma unroll
       for (int eg = 0; eg < NE; ++eg)
 #pragma unroll
@@ -251,6 +262,7 @@ __device__ __forceinline__ void attend(unsigned char* smem, const Item& C, const
         const bf16x2_t h = __builtin_convertvector(e, bf16x2_t);
         pf[j][r] = h[0];
         pf[j][r + 1] = h[1];
+        if (LSE) lx += e[0] + e[1];
         if constexpr (Keys::kPaged)
           ls += e[0] + e[1];
         else
@@ -278,14 +290,8 @@ __device__ __forceinline__ void attend(unsigned char* smem, const Item& C, const
       }
   }
   vm_wait<0>();  // loads issued for tiles past the last one
-  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(ls), __float_as_uint(ls), false, false);
-  ls = __uint_as_float(both[0]) + __uint_as_float(both[1]);
-}
-
-// The log of a row's sum of exponentials (natural), from its reference m in log2
-// units and its sum ls over exp2(score - m): the sum that O is divided by.
-__device__ __forceinline__ float row_lse(float m, float ls) {
-  return (m + log2f(ls)) * 0.6931471805599453f;
+  ls = add_xor32(ls);
+  if (LSE) lx = row_lse(m_run, add_xor32(lx));
 }
 
 // LSE: rows' log sums go to lse [B][H][nq] too.
@@ -341,10 +347,10 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
     }
   }
   f32x16_t o[DH / 32];
-  float ls, m;
+  float ls, lx;
   const SeqKeys<DH> keys{K + (size_t)C.bh * ldk * DH, V + (size_t)C.bh * ldk * DH};
-  attend<DH, S, NW>(smem, C, keys, rs, qf, c2, o, ls, m);  // ls >= 1 for a valid row: its maximum's term
-  if (LSE && valid && lane < 32) lse[(size_t)C.bh * nq + row] = row_lse(m, ls);
+  attend<DH, S, NW, LSE>(smem, C, keys, rs, qf, c2, o, ls, lx);  // ls >= 1 for a valid row: its maximum's term
+  if (LSE && valid && lane < 32) lse[(size_t)C.bh * nq + row] = lx;
 
   // O: [B][H][nq][DH], or [B][nq][H][DH] (rows of a residual stream) with o_inter
   const int ob = C.bh / H, oh = C.bh - ob * H;
@@ -393,10 +399,10 @@ __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH
   }
   if (valid) rs.hi[0] = ctx + row + 1;
   f32x16_t o[DH / 32];
-  float ls, m;
+  float ls, lx;
   const PagedKeys<DH> keys{kv, kg, __builtin_amdgcn_readfirstlane(g.slot(b)),
                            kg.head_off(layer, 0, h), kg.head_off(layer, 1, h), ctx + g.R};
-  attend<DH, S, NW>(smem, C, keys, rs, qf, c2, o, ls, m);
+  attend<DH, S, NW>(smem, C, keys, rs, qf, c2, o, ls, lx);
   store_row<DH>(O + at, valid, o, 1.0f / ls);
 }
 
@@ -417,6 +423,11 @@ __device__ inline int swz16(int r) {
 __device__ inline float max_xor16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ inline float add_xor16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 template <int DH, int S, bool LSE>
@@ -502,6 +513,7 @@ __global__ void __launch_bounds__(256)
   // P, formed by the MFMA against a block of ones (each element of ls is the
   // sum of this lane's query row over the bf16 probabilities that o uses)
   float m_run = -INFINITY;
+  float lx = 0.f;  // this lane's part of the sum over the fp32 ones (see attend())
   f32x4_t o[NDB], ls = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < NDB; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -573,6 +585,7 @@ __global__ void __launch_bounds__(256)
         const float mn = grow ? mx : m_run;
         const float alpha = __builtin_amdgcn_exp2f(m_run - mn);
         ls *= alpha;
+        if (LSE) lx *= alpha;
 #pragma unroll
         for (int db = 0; db < NDB; ++db) o[db] *= alpha;
         m_run = mn;
@@ -582,9 +595,11 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
       for (int gg = 0; gg < 4; ++gg)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          pf[gg >> 1][4 * (gg & 1) + r] =
-              (bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[gg][r], c2, -mref));
+        for (int r = 0; r < 4; ++r) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[gg][r], c2, -mref));
+          pf[gg >> 1][4 * (gg & 1) + r] = (bf16)e;
+          if (LSE) lx += e;
+        }
       ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[0], ls, 0, 0, 0);
       ls = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[1], ls, 0, 0, 0);
       // O^T += V^T P^T, keys 0..31 then 32..63
@@ -603,10 +618,11 @@ __global__ void __launch_bounds__(256)
   }
   vm_wait<0>();  // loads issued for tiles past the last one
 
+  if (LSE) lx = row_lse(m_run, add_xor32(add_xor16(lx)));
   // lane: query lq, d_head 16db + 4gq + r
   if (valid) {
     const float inv = __builtin_amdgcn_rcpf(ls[0]);  // ls >= 1: the row maximum's term
-    if (LSE && gq == 0) lse[(size_t)C.bh * nq + row] = row_lse(m_run, ls[0]);
+    if (LSE && gq == 0) lse[(size_t)C.bh * nq + row] = lx;
     // O: [B][H][nq][DH], or [B][nq][H][DH] (rows of a residual stream) with o_inter
     const int ob = C.bh / H, oh = C.bh - ob * H;
     bf16* orow = O + (o_inter ? (((size_t)ob * nq + row) * H + oh) * DH
