@@ -349,9 +349,10 @@ int kf_training_attention_lse(void *hip_stream, int mask, int B, int H, int N, i
  * O and lse are the forward call's, dO the gradient of O; dQ, dK and dV are
  * written whole and must not overlap the inputs or each other.  Layouts, types
  * (bf16; lse fp32), alignment, limits and errors as in kf_training_attention;
- * P and dS enter the matrix products in bf16 (dS for dQ as two bf16 terms; P and
- * dS for dV and dK likewise where there are few rows), all sums are fp32 and of a
- * fixed order (no atomics: a call's result is the same on every run).
+ * P and dS enter the matrix products as two bf16 terms each, their rounding and
+ * the rest, whatever B and H; all sums are fp32 and of a fixed order (no atomics:
+ * a call's result is the same on every run).  O enters D as it was rounded, which
+ * is mended exactly for dK and dV, and for dQ where blocks of rows see few keys.
  * Inputs are finite: an infinity or NaN may spread to rows and keys of its head
  * that do not see it.  scale in [1e-20, 1e20], keys * k below 2^32, blocks of
  * 128 keys (the context's and each noise region's by themselves) of all heads

@@ -14,32 +14,32 @@
 //     that makes a row of dS sum to zero, so D + (the fp32 sum of that row) is stored.
 //     In dQ itself D's error counts where a row sees few keys (it falls with the root of
 //     their number against dS): blocks with such rows, short walks, take that sum in a
-//     walk of its own first.  dQ of N = 2, k = 1 M_D is off by 1.9e-3 instead of 3.6e-3, of
-//     N = 16, k = 4 by 1.7e-3 instead of 2.2e-3; forward and backward of M_S, 768 heads,
-//     k = 4 take 41 us instead of 38 at N = 16, 225 instead of 219 at N = 128.  For every
-//     row, by P K beside the walk, it takes 32 registers more and two wavefronts per SIMD
-//     instead of three (M_D at N = 1024: 171 us against 154).
-//     dS enters the product as two bf16 terms, its rounding and the rest.
+//     walk of its own first.  Without it dQ of N = 2, k = 1 M_D is off by 2.9e-3 instead
+//     of 1.7e-3, of N = 16, k = 4 by 2.1e-3 instead of 1.7e-3; forward and backward of M_S,
+//     768 heads, k = 4 take 43 us instead of 40 at N = 16, 239 instead of 232 at N = 128.
+//     For every row, by P K beside the walk, it takes 32 registers more and two wavefronts
+//     per SIMD instead of three (M_D at N = 1024: 171 us, this 154 in the same run).
 //   dK, dV: a workgroup owns 128 keys of one key region and walks the query rows
 //     that see them: at most two row intervals, the mask read by columns.  Scores
 //     are formed as queries x keys, a lane holds one key, and P and dS are the B
 //     operands of dV^T += dO^T P and dK^T += Q^T dS.
-// On small grids (FINE) P and dS enter dV and dK as two terms as well.  Errors against 64
-// bits (norms; the results' own rounding is 1.7e-3): dQ 1.7e-3 to 2.0e-3, dK and dV
-// 2.4e-3, on small grids 1.8e-3.  One term everywhere and D as it comes took dQ and dK to
-// 2.5e-3 to 2.8e-3; two terms everywhere take dK and dV of M_D at N = 1024 from 209 to
-// 270 us.
+// P and dS enter their products as two bf16 terms, the rounding and the rest.  Errors
+// against 64 bits (norms; the results' own rounding is 1.66e-3): dK and dV 1.66e-3, dQ
+// 1.66e-3 to 1.71e-3 (D's error in blocks that see many keys).  One term in dV and dK takes
+// them to 2.3e-3; forward and backward of M_D at N = 1024 then take 412 us instead of 475,
+// of M_S at N = 128 227 instead of 238, other shapes 0 to 13 % less.  Two terms whatever
+// the grid: a head's gradients are as good among many heads as alone.
 // Together the walks form scores and dO V^T twice: 8 products of the visible pairs, where
 // a single walk that adds dQ with atomics would form 5 or 6.
 // Operands that a product needs with the other index first come through the
 // transposing LDS reads of the same tiles.
 //
-// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 159 us, dK and dV 211 (352 TFLOP/s of the
+// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 159 us, dK and dV 274 (298 TFLOP/s of the
 // 5 products of the visible pairs).  Neither bytes nor matrix rate bound it but latency:
-// a wavefront's chain from LDS through two products, the exponential and two more, with
+// a wavefront's chain from LDS through two products, the exponential and four more, with
 // the 3 (dQ) and 2 (dK, dV) wavefronts a SIMD that the registers allow.  M_S, 768 heads,
-// N = 128: 86 and 88 us for 385 MB each (Q, K, V, dO are read by both walks), 4.5 and 4.4
-// TB/s: memory bounds it.
+// N = 128: 87 and 102 us for 385 MB each (Q, K, V, dO are read by both walks), 4.4 and 3.8
+// TB/s: memory bounds the one, memory and the chain the other.
 #include "kf_blockattn.h"
 #include "kf_route.h"
 #include "kf_train.h"
@@ -376,7 +376,7 @@ struct KvGeo : Geo<DH, S, 4> {
 // accumulators: a matrix step with -1 over their three bf16 pieces.  Reading them from
 // LDS in the accumulators' layout was a third of the kernel's LDS traffic and 32
 // registers.
-template <int DH, int S, int KS, bool FINE>
+template <int DH, int S, int KS>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 64 ? 2 : 1)))
     training_attention_dkv_kernel(BwdArgs a) {
   using G = KvGeo<DH, S>;
@@ -502,19 +502,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 
         s[i] = __builtin_amdgcn_exp2f(s[i] * a.c2);
         dp[i] *= s[i];
       }
-      bf16x8_t p[2], ds[2];
+      bf16x8_t p[2], ds[2], rest[2];
       to_bf16(p, s);
       to_bf16(ds, dp);
       lgkm_wait0();
       mul_tr<DH>(dv, gt, p);
       mul_tr<DH>(dk, qt, ds);
-      if constexpr (FINE) {
-        bf16x8_t rest[2];
-        rest_bf16(rest, s, p);
-        mul_tr<DH>(dv, gt, rest);
-        rest_bf16(rest, dp, ds);
-        mul_tr<DH>(dk, qt, rest);
-      }
+      rest_bf16(rest, s, p);
+      mul_tr<DH>(dv, gt, rest);
+      rest_bf16(rest, dp, ds);
+      mul_tr<DH>(dk, qt, rest);
     });
   }
   vm_wait<0>();
@@ -545,10 +542,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DH <= 
   store_row<DH>(a.dK + gkey * DH, valid, dk, a.scale);
 }
 
-template <int DH, int SK, int KS, bool FINE>
+template <int DH, int SK, int KS>
 void launch_dkv(const BwdArgs& a, hipStream_t s) {
   const int nb = (int)backward_key_blocks(a.mask == KF_MASK_DOUBLE, a.N, a.k, 32 * KS);
-  launch((training_attention_dkv_kernel<DH, SK, KS, FINE>), dim3((unsigned)(a.BH * nb)), dim3(256), 0, s, a);
+  launch((training_attention_dkv_kernel<DH, SK, KS>), dim3((unsigned)(a.BH * nb)), dim3(256), 0, s, a);
 }
 
 template <int DH, int S, int SK>
@@ -556,12 +553,10 @@ hipError_t launch_bwd(const BwdArgs& a, hipStream_t s) {
   constexpr int NW = 4;
   const int nqb = (int)backward_row_blocks(a.mask == KF_MASK_DOUBLE, a.N, a.k);
   launch((training_attention_dq_kernel<DH, S, NW>), dim3((unsigned)(a.BH * nqb)), dim3(64 * NW), 0, s, a);
-  if (a.BH * nqb <= 128)
-    launch_dkv<DH, SK, 2, true>(a, s);
-  else if (backward_keys(DH, a.BH, a.N) == 64)
-    launch_dkv<DH, SK, 2, false>(a, s);
+  if (backward_keys(DH, a.BH, a.N) == 64)
+    launch_dkv<DH, SK, 2>(a, s);
   else
-    launch_dkv<DH, SK, 4, false>(a, s);
+    launch_dkv<DH, SK, 4>(a, s);
   return hipGetLastError();
 }
 
