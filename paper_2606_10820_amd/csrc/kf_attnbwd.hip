@@ -34,7 +34,7 @@
 // Operands that a product needs with the other index first come through the
 // transposing LDS reads of the same tiles.
 //
-// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 159 us, dK and dV 274 (298 TFLOP/s of the
+// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 159 us, dK and dV 274 (300 TFLOP/s of the
 // 5 products of the visible pairs).  Neither bytes nor matrix rate bound it but latency:
 // a wavefront's chain from LDS through two products, the exponential and four more, with
 // the 3 (dQ) and 2 (dK, dV) wavefronts a SIMD that the registers allow.  M_S, 768 heads,

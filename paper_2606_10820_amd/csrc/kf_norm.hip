@@ -397,7 +397,7 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
   });
 }
 
-int norm_grad_strips(int64_t rows, int d) { return (int)(rows < kStrips ? rows : kStrips); }
+int norm_grad_strips(int64_t rows) { return (int)(rows < kStrips ? rows : kStrips); }
 
 hipError_t launch_norm_grad(const NormGradArgs& args, hipStream_t s) {
   return by_types(args.x_dtype, args.y_dtype, [&](auto x, auto y) {

@@ -139,18 +139,5 @@ __device__ __forceinline__ S block_add(S v, S* part) {
   }
   return v;
 }
-template <int NW>
-__device__ __forceinline__ float block_max(float v, float* part) {
-  v = wave_max(v);
-  if constexpr (NW > 1) {
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = part[0];
-#pragma unroll
-    for (int i = 1; i < NW; ++i) v = fmaxf(v, part[i]);
-    __syncthreads();
-  }
-  return v;
-}
 
 }  // namespace kf

@@ -38,7 +38,7 @@ struct NormGradArgs {
   float* part;
 };
 // Row strips whose column sums reach the workspace as partial results.
-int norm_grad_strips(int64_t rows, int d);
+int norm_grad_strips(int64_t rows);
 hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t s);
 
 struct LogprobArgs {

@@ -169,7 +169,7 @@ int kf_layer_norm(void* hip_stream, int norm, int x_dtype, int y_dtype, int64_t 
 
 size_t kf_layer_norm_backward_bytes(int64_t rows, int d) {
   if (rows <= 0 || d < 1 || d > kMaxWidth) return 0;
-  return (size_t)kf::norm_grad_strips(rows, d) * 2 * d * sizeof(float);
+  return (size_t)kf::norm_grad_strips(rows) * 2 * d * sizeof(float);
 }
 
 int kf_layer_norm_backward(void* hip_stream, int norm, int x_dtype, int y_dtype, int64_t rows,
