@@ -424,7 +424,9 @@ int kf_layer_norm_backward(void *hip_stream, int norm, int x_dtype, int y_dtype,
  *   tokens int32 [rows], or null: no row has a token.  A negative token is a
  *   row without one (logp 0); a token >= vocab gives logp NaN.
  *   logp, entropy, lse: fp32 [rows], each may be null.
- *   1 <= vocab <= 2^28, 0 <= n_top <= min(vocab, KF_MAX_TOP).
+ *   1 <= vocab <= 2^28, 0 <= n_top <= min(vocab, KF_MAX_TOP).  More than 56
+ *   alternatives, or more than the ids that a finite mask value leaves, take up
+ *   to a hundred times as long (8192 x 30522: 0.2 ms for 56, 11 for 64).
  * Logits of minus infinity have probability 0.  A row of nothing else has lse,
  * logp and top_logp minus infinity and entropy 0.  NaN or plus infinity in a
  * row makes its results NaN (ids stay those of the order above). */

@@ -420,7 +420,9 @@ def training_attention(mask: int, q, k_, v, N: int, k: int, scale: Optional[floa
 
 # ------------------------------------------------ operators of the training step
 # Each call runs on `stream` (default: torch's current stream of the tensors'
-# device) and allocates its results there.
+# device) and allocates its results there.  The calls are no part of autograd:
+# their results carry no graph, also where an argument requires gradients, and
+# the *_backward functions are called by the training loop itself.
 
 _NOTHING = contextlib.nullcontext()
 
@@ -519,7 +521,7 @@ def _attention_args(mask, q, k_, v, N, k, *more):
 def training_attention_lse(mask: int, q, k_, v, N: int, k: int, scale: Optional[float] = None,
                            stream=None):
     """training_attention that also returns each query row's log of the sum of exponentials,
-    (out, lse [B][H][rows] fp32), for training_attention_backward."""
+    (out, lse [B][H][rows] fp32), for training_attention_backward (no autograd graph)."""
     import torch
     B, H, rows, dh = _attention_args(mask, q, k_, v, N, k)
     s, ctx = _on(q.device, stream, (q, k_, v))
@@ -556,7 +558,8 @@ def layer_norm(x, gain, shift=None, eps: float = 1e-5, rms: bool = False, out_dt
     """LayerNorm (or with rms RMSNorm) of the rows of x [..., d] (kf_layer_norm).
 
     gain, shift [d] fp32.  Returns (y, stats): y like x in out_dtype (default x's;
-    another only for fp32 x), stats [rows][2] fp32 for layer_norm_backward."""
+    another only for fp32 x), stats [rows][2] fp32 for layer_norm_backward (no autograd
+    graph)."""
     import torch
     rows, ldx = _rows(x, "x")
     d, dev = x.shape[-1], x.device
@@ -619,7 +622,8 @@ class TokenLogprobs(NamedTuple):
 def token_logprobs(logits, tokens=None, n_top: int = 0, entropy: bool = True, lse: bool = False,
                    stream=None) -> TokenLogprobs:
     """Log probabilities of tokens [...] int32 under softmax(logits [..., vocab]), with the
-    rows' entropies, log-sums (lse) and n_top most probable ids (kf_token_logprobs)."""
+    rows' entropies, log-sums (lse) and n_top most probable ids (kf_token_logprobs; no
+    autograd graph)."""
     import torch
     rows, ld = _rows(logits, "logits")
     lead, V, dev = logits.shape[:-1], logits.shape[-1], logits.device

@@ -11,8 +11,9 @@
 //
 // Bound by memory, n read twice (the scale is known only after the last gradient; what
 // the caches keep of the first read is the only saving): 130 M gradients, bf16 into fp32,
-// 43 us for the norm (6.1 TB/s) and 115 for the scaled copy (6.8).  A small model's 30
-// tensors are bound by the two launches (3 + 4 us).
+// 43 us for the norm (6.1 TB/s) and 115 for the scaled copy (6.8).  Tensors that do not begin
+// at a multiple of 16 bytes go element by element: norm 59 us instead of 44, both together
+// 325 instead of 163.  A small model's 30 tensors are bound by the two launches (3 + 4 us).
 #include <type_traits>
 
 #include "kf_rows.h"

@@ -10,9 +10,11 @@
 //
 // Bound by memory where the rows are many: 8192 x 50257 bf16 with the gradient 306 us
 // (5.4 TB/s), 1003 x 30522 fp32 with the entropy's 47 (5.2, in the caches in part), the
-// sums alone of 8192 x 30522 bf16 95 (5.3).  The alternatives cost that case 10 to 20 us
-// more: a bound on the n-th largest, then a look at what passes it.  Few rows (4 x 50257)
-// are bound by one workgroup's read of a row and its rounds of reductions, 10 us.
+// sums alone of 8192 x 30522 bf16 90 (5.5).  The alternatives, a bound on the n-th largest
+// and a look at what passes it, take that case to 113 us for 8, 149 for 32 and 209 for 56.
+// Beyond that more elements pass than are kept (see kTopCap): 1.1 ms for 58, 3.8 for 62,
+// 11.4 for 64.  Few rows (4 x 50257) are bound by one workgroup's read of a row and its
+// rounds of reductions, 10 us.
 #include "kf_lds.h"
 #include "kf_rows.h"
 #include "kf_train.h"
@@ -132,7 +134,10 @@ struct Raw<f16> {
   }
 };
 
-constexpr int kTopCap = 256;  // alternatives' candidates kept in LDS
+// Alternatives' candidates kept in LDS.  The n-th of 64 sets' maxima is passed by about
+// 64 (1 / 64 + 1 / 63 + ... + 1 / (65 - n)) elements of unordered logits: 8.5 for n = 8, 130 for 56,
+// 208 for 62, 304 for 64.
+constexpr int kTopCap = 256;
 
 // One row's LDS.
 template <int NT>
@@ -324,7 +329,9 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
         // bound that n_top of the sets' maxima reach is one that the n_top largest
         // elements reach.  The elements that reach it, few beyond n_top, are ranked
         // against each other.  A row with NaN or plus infinity (s is NaN) or with too many
-        // of them (equal logits) goes the long way.
+        // of them goes the long way: n of 58 and more on ordinary rows, and rows where fewer
+        // than n sets hold anything above a value that most share (equal logits, a
+        // vocabulary masked by a finite value down to fewer than n ids).
         const int n = a.n_top;
         float v = tm;
         if constexpr (NW > 1) {

@@ -13,7 +13,12 @@
 // Bound by memory: a row is read once, kept in the registers of as many lanes as it
 // fills (a second read, from L2, costs as much as the first), and written once.
 // Forward 40 us at 40960 x 768 fp32 to bf16 (4.7 TB/s) and 58 at 81920 x 1024 bf16
-// (5.8), backward with dres 66 (6.6, x in part from the caches) and 114 (5.9).  A few rows are bound by the launch (2.8 us).
+// (5.8), backward with dres 66 (6.6, x in part from the caches) and 114 (5.9).  A few rows
+// are bound by the launch (2.8 us).  Widths that are not whole vectors of 16 bytes take single
+// elements: 40000 x 771 against 768, forward and backward, 31 and 78 us against 29 and 71
+// (fp32 to bf16), 37 and 61 against 25 and 52 (bf16: twice the elements a lane).  Rows of more
+// than 8192 columns are read three times, an element at a time: 4096 x 16384 bf16 131 and
+// 334 us (2.1 and 1.6 TB/s) against 24 and 65 at 4096 x 8192.
 #include <type_traits>
 
 #include "kf_rows.h"
