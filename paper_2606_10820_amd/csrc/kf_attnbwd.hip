@@ -29,16 +29,16 @@
 // them to 2.3e-3; forward and backward of M_D at N = 1024 then take 412 us instead of 475,
 // of M_S at N = 128 227 instead of 238, other shapes 0 to 13 % less.  Two terms whatever
 // the grid: a head's gradients are as good among many heads as alone.
-// Together the walks form scores and dO V^T twice: 8 products of the visible pairs, where
-// a single walk that adds dQ with atomics would form 5 or 6.
+// Together the walks form scores and dO V^T twice: 10 products of the visible pairs, where
+// a single walk would form 8, with atomics for dQ or a head's context in one workgroup.
 // Operands that a product needs with the other index first come through the
 // transposing LDS reads of the same tiles.
 //
-// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 159 us, dK and dV 274 (300 TFLOP/s of the
+// M_D, 48 heads, N = 1024, k = 4, d_head 64: dQ 154 us, dK and dV 260 (314 TFLOP/s of the
 // 5 products of the visible pairs).  Neither bytes nor matrix rate bound it but latency:
 // a wavefront's chain from LDS through two products, the exponential and four more, with
 // the 3 (dQ) and 2 (dK, dV) wavefronts a SIMD that the registers allow.  M_S, 768 heads,
-// N = 128: 87 and 102 us for 385 MB each (Q, K, V, dO are read by both walks), 4.4 and 3.8
+// N = 128: 86 and 101 us for 385 MB each (Q, K, V, dO are read by both walks), 4.5 and 3.8
 // TB/s: memory bounds the one, memory and the chain the other.
 #include "kf_blockattn.h"
 #include "kf_route.h"
