@@ -68,9 +68,14 @@ inline long long training_groups(int dh, long long BH, bool two_parts, long long
 // Its gradients: workgroups of the dQ walk, 128 query rows each (M_D's halves by
 // themselves), and keys of a workgroup of the dK, dV walk.  64, its rows in two groups,
 // where there are few blocks of 128 context keys (the long ones); 128 otherwise.  us of
-// both walks, 64 | 128 keys, by the number of those blocks: d_head 64 48 57 | 68, 96
-// 154 | 186, 192 81 | 88 and 181 | 215, 288 240 | 244, 384 313 | 283; d_head 32 96
-// 26 | 30, 192 40 | 39; d_head 128 96 87 | 99, 192 161 | 130.
+// both walks, 64 | 128 keys, k = 4, by the number of those blocks (M_S with N = 128, M_S
+// and M_D with N = 1024):
+//   d_head 32   48 23 | 27, 92 | 122, 134 | 181    192 41 | 39, 114 | 144, 164 | 211
+//               384 63 | 64, 150 | 175, 233 | 265
+//   d_head 64   48 30 | 34, 118 | 153, 171 | 228   192 60 | 60, 152 | 187, 221 | 273
+//               384 101 | 95, 227 | 230, 390 | 371
+//   d_head 128  48 44 | 54, 192 | 257, 291 | 392   96 70 | 72, 205 | 272, 315 | 419
+//               192 117 | 107, 272 | 315, 444 | 487   384 240 | 207, 514 | 433, 876 | 729
 inline long long backward_row_blocks(bool two_parts, long long N, long long k) {
   return two_parts ? 2 * ((N * k + 127) / 128) : (N + N * k + 127) / 128;
 }
