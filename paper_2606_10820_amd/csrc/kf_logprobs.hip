@@ -25,8 +25,8 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // exp2 of this and of anything below is zero.  Differences from the maximum (log2 units,
 // minus infinity for a masked logit) are raised to it where they are a factor beside that
-// exponential: the product is then zero whatever the entropy's weight (a factor of size 3e38
-// overflowed from weights of 1.64 on, and zero times infinity is NaN).
+// exponential: the product is then zero for entropy weights up to 1e36 (a factor of size
+// 3e38 overflowed from weights of 1.64 on, and zero times infinity is NaN).
 constexpr float kNoShare = -256.f;
 
 // Order of the alternatives: larger logits first, equal ones by the lower id; NaN
