@@ -450,6 +450,125 @@ int kf_token_logprobs_backward(void *hip_stream, int dtype, int64_t rows, int vo
                                const float *d_logp, const float *d_entropy, float *logp,
                                float *entropy, float *lse, void *d_logits, int64_t ldd);
 
+/* Rows of a QKV product into the layout of kf_training_attention, with an RMS norm of
+ * each query and key head and rotary positions.  x [B * L][(n_head + 2 n_kv) d_head] of
+ * x_dtype, ldx apart: a row's query heads, key heads, value heads.  For query and key
+ * heads, with g = q_gain or k_gain,
+ *     n = x r g,  r = 1 / sqrt(mean(x^2) + eps)      (gain null: n = x)
+ *     (y_2i, y_2i+1) = (c n_2i - s n_2i+1, s n_2i + c n_2i+1),  2i < d_rot
+ * with (c, s) = table[position][i], fp32 [n_pos][d_rot / 2][2] (kf_rope_table; the
+ * paper's backbone has d_rot = min(64, d_head)); columns from d_rot on, and with
+ * d_rot 0 all of them, are not turned.  Value heads are copied.
+ *   positions int32: row (b, l) is at positions[b * pos_ld + l] (pos_ld 0: one list of
+ *   L for all sequences), or null: at l.  A position outside [0, n_pos) gives NaN in the
+ *   turned columns.
+ *   q, k, v: where head h of row (b, l) goes, d_head consecutive elements of y_dtype at
+ *   ptr + b batch + h head + l row (a view of a larger tensor will do, as a region of
+ *   KF_MASK_DOUBLE's keys); heads must not share elements; a null ptr: not wanted.
+ *   x_dtype and y_dtype are equal, or x_dtype is fp32.
+ * 0 <= B, L (either 0: nothing launched), B * L <= 2^30, 0 <= n_head, n_kv with 1 to 65536
+ * heads of all three kinds, 1 <= d_head <= KF_MAX_HEAD, d_rot even, 0 <= d_rot <= d_head,
+ * eps >= 0 and finite.  Results must not overlap x or each other. */
+#define KF_MAX_HEAD 512
+typedef struct kf_heads {
+  void *ptr;
+  int64_t batch, head, row; /* elements, >= 0 */
+} kf_heads;
+int kf_qkv_heads(void *hip_stream, int x_dtype, int y_dtype, int B, int L, int n_head, int n_kv,
+                 int d_head, const void *x, int64_t ldx, const float *q_gain, const float *k_gain,
+                 float eps, const float *table, int n_pos, int d_rot, const int32_t *positions,
+                 int64_t pos_ld, const kf_heads *q, const kf_heads *k, const kf_heads *v);
+
+/* Gradients of kf_qkv_heads: dq, dk, dv of y_dtype (any strides >= 0: an expanded gradient
+ * will do; a null ptr: zeros) into dx of x_dtype, rows like x's, written whole; with w the
+ * turn of dy by the opposite angle,
+ *     dx = r (w g - x r mean(w g x r)),  dgain = sum over rows and heads of w x r
+ * (gain null: dx = w).  x may be null where no head has a gain; dx may be x (with its ld).
+ * dq_gain, dk_gain fp32 [d_head] are written, not added to; either may be null (each must be
+ * where its gain is), and with both null no workspace is needed.  With B or L 0 they become zeros.
+ * workspace: kf_qkv_heads_backward_bytes() bytes of device memory, 16-byte aligned, used
+ * during the call only; calls that overlap need one each. */
+size_t kf_qkv_heads_backward_bytes(int B, int L, int n_head, int n_kv, int d_head);
+int kf_qkv_heads_backward(void *hip_stream, int x_dtype, int y_dtype, int B, int L, int n_head,
+                          int n_kv, int d_head, const kf_heads *dq, const kf_heads *dk,
+                          const kf_heads *dv, const void *x, int64_t ldx, const float *q_gain,
+                          const float *k_gain, float eps, const float *table, int n_pos, int d_rot,
+                          const int32_t *positions, int64_t pos_ld, void *dx, int64_t lddx,
+                          float *dq_gain, float *dk_gain, void *workspace, size_t workspace_bytes);
+
+/* table[p][i] = (cos, sin) of p base^(-2i / d_rot), fp32 [n_pos][d_rot / 2][2] from angles in
+ * fp64.  1 <= n_pos, d_rot even and in [2, KF_MAX_HEAD], base > 0 and finite; table 8-byte aligned. */
+int kf_rope_table(void *hip_stream, int n_pos, int d_rot, double base, float *table);
+
+/* Dropout, added to a residual where one is given:
+ *     y = res + [kept] x s,   s = 1 / (1 - p')
+ * The mask is a function of (seed, site, row, column) alone, never stored: Philox4x32-10 with
+ * the seed as its key and counter (column / 8, row, row / 2^32, 2^31 + site) gives eight
+ * columns' 16-bit numbers (word j: columns 2j, low half, and 2j + 1); an element is dropped
+ * where its number is below p' 65536, the nearest whole number to p 65536.  A dropped
+ * element counts 0 whatever it holds; p = 0 drops nothing, p = 1 everything (s = 0).
+ *   x [rows][d] of x_dtype, y of y_dtype: equal types, or either of them fp32; res (null:
+ *   none) of y_dtype.  y may be x (equal types and ld) or res (its ld); otherwise they must
+ *   not overlap.
+ *   seed, site: a call's own (site below 2^31: a layer, a step); dev_seed (null: none) is a
+ *   number in device memory, 8-byte aligned, that is added to seed when the kernel runs, so
+ *   that a captured call has another mask on each replay.
+ * 1 <= d <= 2^28, 0 <= rows (0: nothing launched), 0 <= p <= 1. */
+int kf_dropout(void *hip_stream, int x_dtype, int y_dtype, int64_t rows, int d, const void *x,
+               int64_t ldx, const void *res, int64_t ldres, float p, uint64_t seed,
+               const uint64_t *dev_seed, uint32_t site, void *y, int64_t ldy);
+/* Its gradient dx = [kept] dy s, of x_dtype from dy of y_dtype (the gradient of res is dy);
+ * dx may be dy (equal types and ld). */
+int kf_dropout_backward(void *hip_stream, int x_dtype, int y_dtype, int64_t rows, int d,
+                        const void *dy, int64_t lddy, float p, uint64_t seed,
+                        const uint64_t *dev_seed, uint32_t site, void *dx, int64_t lddx);
+
+/* The joint of a pre-norm block in one pass: h = res + dropout(x) and y = norm(h), the results of
+ * kf_dropout and kf_layer_norm one after the other (bit for bit where the rows of all
+ * tensors are aligned alike; the order of a row's sums goes by it).  x and y are of y_dtype (a
+ * product's), res and h of h_dtype: equal types, or h_dtype fp32.  h may be res (its ld);
+ * otherwise nothing overlaps.  The rest as in those two. */
+int kf_dropout_norm(void *hip_stream, int norm, int h_dtype, int y_dtype, int64_t rows, int d,
+                    const void *x, int64_t ldx, const void *res, int64_t ldres, float p,
+                    uint64_t seed, const uint64_t *dev_seed, uint32_t site, const float *gain,
+                    const float *shift, float eps, void *h, int64_t ldh, void *y, int64_t ldy,
+                    float *stats);
+/* Its gradients: dh (of h_dtype, also the gradient of res) is kf_layer_norm_backward's dx with
+ * dres, and dx (of y_dtype) kf_dropout_backward's of dh, as above.  dh may be dres (its ld);
+ * otherwise nothing overlaps.  workspace as in kf_layer_norm_backward. */
+int kf_dropout_norm_backward(void *hip_stream, int norm, int h_dtype, int y_dtype, int64_t rows,
+                             int d, const void *dy, int64_t lddy, const void *h, int64_t ldh,
+                             const float *gain, const float *stats, const void *dres,
+                             int64_t lddres, float p, uint64_t seed, const uint64_t *dev_seed,
+                             uint32_t site, void *dh, int64_t lddh, void *dx, int64_t lddx,
+                             float *dgain, float *dshift, void *workspace, size_t workspace_bytes);
+
+/* The clipped policy loss of sampled tokens with a KL term and an entropy bonus, and its
+ * gradient, from logits [rows][vocab] of dtype.  For a row with a token t,
+ *     logp = l_t - lse,  ratio = exp(logp - old_logp)      (old_logp null: 1, on policy)
+ *     kl = e^g - g - 1,  g = ref_logp - logp               (ref_logp null: none)
+ *     row_loss = weight (-min(ratio A, clip(ratio, clip_low, clip_high) A) + kl_coef kl
+ *                        - entropy_coef entropy)           (weight null: 1)
+ * with A = advantage[row], and loss, one number, the sum of row_loss (formed in fp64).  The
+ * gradient with u = -ratio A where ratio A is the lesser (or equal), else 0, less kl_coef (e^g - 1):
+ *     d_logits[v] = weight (u ([v = t] - p_v) + entropy_coef p_v (log p_v + entropy))
+ * tokens int32 [rows].  A row whose token is negative or whose weight is 0 counts nothing: every
+ * result of it is 0, whatever its logits hold; they are not read.  A token >= vocab gives NaN.
+ * A token of logit minus infinity has logp minus infinity, ratio 0 and, with a reference, kl
+ * plus infinity.  advantage, old_logp, ref_logp, weight: fp32 [rows].
+ *   row_loss fp32 [rows] is written always; logp, ratio, kl (needs ref_logp), entropy fp32
+ *   [rows] and loss fp32 [1] each may be null.
+ *   d_logits (null: no gradient) of dtype, ldd apart; it may be logits (ldd = ld), otherwise
+ *   they must not overlap.
+ * 0 <= clip_low <= 1 <= clip_high (infinity: not clipped), kl_coef and entropy_coef finite and
+ * at most 1e18 in size, 1 <= vocab <= 2^28, 0 <= rows (0: loss becomes 0). */
+int kf_policy_loss(void *hip_stream, int dtype, int64_t rows, int vocab, const void *logits,
+                   int64_t ld, const int32_t *tokens, const float *advantage,
+                   const float *old_logp, const float *ref_logp, const float *weight,
+                   float clip_low, float clip_high, float kl_coef, float entropy_coef,
+                   float *row_loss, float *logp, float *ratio, float *kl, float *entropy,
+                   float *loss, void *d_logits, int64_t ldd);
+
 /* The norm of a model's whole gradient and its clipping, over any number of
  * tensors.  Each holds n consecutive elements src of src_dtype; the scaled
  * gradient goes to dst: of the same type, or fp32 (half-precision gradients

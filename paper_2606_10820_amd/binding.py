@@ -54,6 +54,11 @@ class KfGradPlan(ctypes.Structure):
     _fields_ = [("dev", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("has_dst", ctypes.c_int)]
 
 
+class KfHeads(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64),
+                ("row", ctypes.c_int64)]
+
+
 class KfError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"kforcing error {code}: {msg}")
@@ -74,7 +79,8 @@ def lib():
                           "`python -m paper_2606_10820_amd.build` (there is no CPU fallback)")
     L = ctypes.CDLL(_LIB_PATH)
     P, I, U64, SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64, ctypes.c_size_t
-    I64, F = ctypes.c_int64, ctypes.c_float
+    I64, F, U32 = ctypes.c_int64, ctypes.c_float, ctypes.c_uint32
+    HP = ctypes.POINTER(KfHeads)
     CP = ctypes.POINTER(KfConfig)
     IP = ctypes.POINTER(ctypes.c_int)
     sigs = {
@@ -112,6 +118,19 @@ def lib():
                                        P, P, P, SZ]),
         "kf_token_logprobs": (I, [P, I, I64, I, P, I64, P, I, P, P, P, P, P]),
         "kf_token_logprobs_backward": (I, [P, I, I64, I, P, I64, P, P, P, P, P, P, P, I64]),
+        "kf_qkv_heads": (I, [P] + [I] * 7 + [P, I64, P, P, F, P, I, I, P, I64, HP, HP, HP]),
+        "kf_qkv_heads_backward_bytes": (SZ, [I] * 5),
+        "kf_qkv_heads_backward": (I, [P] + [I] * 7 + [HP, HP, HP, P, I64, P, P, F, P, I, I, P, I64,
+                                                      P, I64, P, P, P, SZ]),
+        "kf_rope_table": (I, [P, I, I, ctypes.c_double, P]),
+        "kf_dropout": (I, [P, I, I, I64, I, P, I64, P, I64, F, U64, P, U32, P, I64]),
+        "kf_dropout_backward": (I, [P, I, I, I64, I, P, I64, F, U64, P, U32, P, I64]),
+        "kf_dropout_norm": (I, [P, I, I, I, I64, I, P, I64, P, I64, F, U64, P, U32, P, P, F, P, I64,
+                                P, I64, P]),
+        "kf_dropout_norm_backward": (I, [P, I, I, I, I64, I, P, I64, P, I64, P, P, P, I64, F, U64, P,
+                                         U32, P, I64, P, I64, P, P, P, SZ]),
+        "kf_policy_loss": (I, [P, I, I64, I, P, I64, P, P, P, P, P, F, F, F, F, P, P, P, P, P, P, P,
+                               I64]),
         "kf_grad_plan_bytes": (SZ, [I, P]),
         "kf_grad_plan_init": (I, [P, I, P, P, SZ, ctypes.POINTER(KfGradPlan)]),
         "kf_grad_norm": (I, [P, ctypes.POINTER(KfGradPlan), P]),
@@ -669,6 +688,306 @@ def token_logprobs_backward(logits, tokens, d_logp=None, d_entropy=None, out=Non
             s, _type(logits.dtype, "logits"), rows, V, logits.data_ptr(), ld, _ptr(tokens),
             _ptr(d_logp), _ptr(d_entropy), logp.data_ptr(), _ptr(H), _ptr(ls), out.data_ptr(), ldd))
     return out, TokenLogprobs(logp, H, ls)
+
+
+def rope_table(n_pos: int, d_rot: int, base: float = 10000.0, device=None, stream=None):
+    """(cos, sin) of position p times base^(-2i / d_rot), fp32 [n_pos][d_rot / 2][2] on `device`
+    (default: the current GPU), for qkv_heads (kf_rope_table); made once."""
+    import torch
+    dev = torch.device("cuda" if device is None else device)
+    if dev.type == "cuda" and dev.index is None:
+        dev = torch.device("cuda", torch.cuda.current_device())
+    if n_pos < 1 or d_rot < 2 or d_rot % 2:
+        raise ValueError("a table has positions and an even number of columns")
+    s, ctx = _on(dev, stream, ())
+    with ctx:
+        table = torch.empty((n_pos, d_rot // 2, 2), dtype=torch.float32, device=dev)
+        _ok(lib().kf_rope_table(s, n_pos, d_rot, base, table.data_ptr()))
+    return table
+
+
+def _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev):
+    """(n_pos, d_rot, pos_ld) of qkv_heads' table and positions."""
+    import torch
+    _check(q_gain, "q_gain", dev, torch.float32, dh)
+    _check(k_gain, "k_gain", dev, torch.float32, dh)
+    n_pos = d_rot = pos_ld = 0
+    if table is not None:
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("table must be [n_pos][d_rot / 2][2] (rope_table)")
+        _check(table, "table", dev, torch.float32, table.numel())
+        n_pos, d_rot = table.shape[0], 2 * table.shape[1]
+    if positions is not None:
+        if positions.shape not in ((L,), (B, L)):
+            raise ValueError("positions must be [L] or [B, L]")
+        _check(positions, "positions", dev, torch.int32, positions.numel())
+        pos_ld = L if positions.dim() == 2 else 0
+    return n_pos, d_rot, pos_ld
+
+
+def _heads_of(t, what, shape, dtype, dev):
+    """t [B][H][L][dh] (or None) as kf_heads."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{what} must be {dtype} {tuple(shape)} on {dev}")
+    sb, sh, sl, sc = t.stride()
+    if sc != 1 and shape[3] > 1:
+        raise ValueError(f"{what}'s last dimension must be contiguous")
+    return KfHeads(t.data_ptr(), sb, sh, sl)
+
+
+def qkv_heads(qkv, n_head: int, n_kv: Optional[int] = None, table=None, positions=None, q_gain=None,
+              k_gain=None, eps: float = 1e-5, out_dtype=None, out=None, stream=None):
+    """Rows of a QKV product, qkv [B, L, (n_head + 2 n_kv) d_head], into attention's layout
+    (kf_qkv_heads): (q [B][n_head][L][d_head], k and v [B][n_kv][L][d_head]).
+
+    q_gain, k_gain [d_head] fp32: an RMS norm of each query and key head.  table (rope_table),
+    positions [L] or [B, L] int32 (default 0..L-1): rotary positions of queries and keys.
+    out: (q, k, v) to write, each a tensor or view of that shape, or None for one that is not
+    wanted.  n_kv defaults to n_head.  No autograd graph."""
+    import torch
+    if qkv.dim() != 3:
+        raise ValueError("qkv must be [B, L, (n_head + 2 n_kv) d_head]")
+    n_kv = n_head if n_kv is None else n_kv
+    B, L, W = qkv.shape
+    H = n_head + 2 * n_kv
+    if n_head < 0 or n_kv < 0 or H < 1 or W % H:
+        raise ValueError("qkv's last dimension must be n_head + 2 n_kv heads")
+    dh, dev = W // H, qkv.device
+    _, ldx = _rows(qkv, "qkv")
+    n_pos, d_rot, pos_ld = _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev)
+    s, ctx = _on(dev, stream, (qkv, table, positions, q_gain, k_gain, *(out or ())))
+    with ctx:
+        if out is None:
+            yt = out_dtype or qkv.dtype
+            out = tuple(torch.empty((B, h, L, dh), dtype=yt, device=dev) for h in (n_head, n_kv, n_kv))
+        else:
+            if len(out) != 3 or all(t is None for t in out):
+                raise ValueError("out must be (q, k, v), one of them at least a tensor")
+            yt = next(t.dtype for t in out if t is not None)
+            if out_dtype not in (None, yt):
+                raise ValueError("out must be of out_dtype")
+        views = [_heads_of(t, n, (B, h, L, dh), yt, dev)
+                 for t, n, h in zip(out, ("q", "k", "v"), (n_head, n_kv, n_kv))]
+        _ok(lib().kf_qkv_heads(s, _type(qkv.dtype, "qkv"), _type(yt, "out"), B, L, n_head, n_kv, dh,
+                               qkv.data_ptr(), ldx, _ptr(q_gain), _ptr(k_gain), eps, _ptr(table),
+                               n_pos, d_rot, _ptr(positions), pos_ld, *views))
+    return tuple(out)
+
+
+def qkv_heads_backward(dq, dk, dv, qkv=None, table=None, positions=None, q_gain=None, k_gain=None,
+                       eps: float = 1e-5, out_dtype=None, out=None, stream=None):
+    """Gradients of qkv_heads (kf_qkv_heads_backward): (dqkv [B, L, (n_head + 2 n_kv) d_head],
+    dq_gain, dk_gain), the last two fp32 [d_head], or None without that gain.
+
+    dq [B][n_head][L][d_head], dk and dv [B][n_kv][L][d_head], of any strides; qkv as in the
+    forward call, needed where there are gains.  dqkv is of qkv's type (without it: out_dtype,
+    default dq's); out: where it goes, qkv itself if that is not needed again."""
+    import torch
+    for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+        if t.dim() != 4:
+            raise ValueError(f"{n} must be [B][heads][L][d_head]")
+    B, Hq, L, dh = dq.shape
+    Hkv, dev = dk.shape[1], dq.device
+    shape = (B, L, (Hq + 2 * Hkv) * dh)
+    ldx, xt = shape[2], out_dtype or (out.dtype if out is not None else dq.dtype)
+    if qkv is not None:
+        _, ldx = _rows(qkv, "qkv", shape)
+        if qkv.device != dev or out_dtype not in (None, qkv.dtype):
+            raise ValueError("qkv must be on dq's device, and dqkv of its type")
+        xt = qkv.dtype
+    elif q_gain is not None or k_gain is not None:
+        raise ValueError("gains' gradients need qkv")
+    n_pos, d_rot, pos_ld = _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev)
+    s, ctx = _on(dev, stream, (dq, dk, dv, qkv, table, positions, q_gain, k_gain, out))
+    with ctx:
+        if out is None:
+            dx, lddx = torch.empty(shape, dtype=xt, device=dev), shape[2]
+        else:
+            dx, (_, lddx) = out, _rows(out, "out", shape)
+            if dx.device != dev or dx.dtype != xt:
+                raise ValueError("out must be of qkv's type and device")
+        views = [_heads_of(t, n, (B, h, L, dh), dq.dtype, dev)
+                 for t, n, h in ((dq, "dq", Hq), (dk, "dk", Hkv), (dv, "dv", Hkv))]
+        dgq, dgk = (torch.empty(dh, dtype=torch.float32, device=dev) if g is not None else None
+                    for g in (q_gain, k_gain))
+        n = lib().kf_qkv_heads_backward_bytes(B, L, Hq, Hkv, dh) if dgq is not None or dgk is not None else 0
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+        _ok(lib().kf_qkv_heads_backward(
+            s, _type(xt, "qkv"), _type(dq.dtype, "dq"), B, L, Hq, Hkv, dh, *views, _ptr(qkv), ldx,
+            _ptr(q_gain), _ptr(k_gain), eps, _ptr(table), n_pos, d_rot, _ptr(positions), pos_ld,
+            dx.data_ptr(), lddx, _ptr(dgq), _ptr(dgk), _ptr(ws), n))
+    return dx, dgq, dgk
+
+
+def _seed(seed, dev):
+    """(host seed, device seed) of an int or of a tensor of one int64 on dev."""
+    if isinstance(seed, int):
+        return seed & 0xFFFFFFFFFFFFFFFF, None
+    import torch
+    _check(seed, "seed", dev, torch.int64, 1)
+    return 0, seed.data_ptr()
+
+
+def dropout(x, p: float, seed, site: int = 0, residual=None, out_dtype=None, out=None, stream=None):
+    """Dropout of the elements of x [..., d] with probability p, the others scaled, added to
+    residual where one is given (kf_dropout).
+
+    The mask is a function of (seed, site, row, column) and is not stored: dropout_backward
+    forms it again from the same seed and site.  seed: an int, or an int64 tensor of one
+    element on the GPU, read when the kernel runs (a captured call then draws another mask
+    each time the tensor has changed).  site: a number below 2^31 for each place that uses the
+    seed.  The result is of residual's type, without one of out_dtype (default x's); out may be
+    residual or x.  No autograd graph."""
+    import torch
+    rows, ldx = _rows(x, "x")
+    d, dev = x.shape[-1], x.device
+    ldres = d
+    yt = out_dtype or (residual.dtype if residual is not None else out.dtype if out is not None else x.dtype)
+    if residual is not None:
+        _, ldres = _rows(residual, "residual", x.shape)
+        if residual.dtype != yt or residual.device != dev:
+            raise ValueError("residual must be of the result's type, on x's device")
+    host, at = _seed(seed, dev)
+    s, ctx = _on(dev, stream, (x, residual, out, None if at is None else seed))
+    with ctx:
+        if out is None:
+            y, ldy = torch.empty(x.shape, dtype=yt, device=dev), d
+        else:
+            y, (_, ldy) = out, _rows(out, "out", x.shape)
+            if y.device != dev or y.dtype != yt:
+                raise ValueError("out must be of the result's type, on x's device")
+        _ok(lib().kf_dropout(s, _type(x.dtype, "x"), _type(yt, "out"), rows, d, x.data_ptr(), ldx,
+                             _ptr(residual), ldres, p, host, at, site, y.data_ptr(), ldy))
+    return y
+
+
+def dropout_backward(dy, p: float, seed, site: int = 0, out_dtype=None, out=None, stream=None):
+    """Gradient of x of dropout from that of its result, dy [..., d] (kf_dropout_backward): of
+    out_dtype (default dy's), out may be dy.  The gradient of residual is dy itself."""
+    return dropout(dy, p, seed, site, None, out_dtype, out, stream)
+
+
+def dropout_norm(x, residual, gain, shift=None, p: float = 0.0, seed=0, site: int = 0,
+                 eps: float = 1e-5, rms: bool = False, out=None, stream=None):
+    """h = residual + dropout(x) and the LayerNorm (or with rms RMSNorm) y of its rows in one pass
+    (kf_dropout_norm): the results of dropout and layer_norm one after the other.
+
+    x [..., d]; residual like x, or fp32.  Returns (h, y, stats): h of residual's type (out: where
+    it goes, residual itself if that is not needed again), y of x's type, stats for
+    dropout_norm_backward.  seed and site as in dropout.  No autograd graph."""
+    import torch
+    rows, ldx = _rows(x, "x")
+    _, ldres = _rows(residual, "residual", x.shape)
+    d, dev = x.shape[-1], x.device
+    if residual.device != dev:
+        raise ValueError("residual must be on x's device")
+    _check(gain, "gain", dev, torch.float32, d)
+    _check(shift, "shift", dev, torch.float32, d)
+    host, at = _seed(seed, dev)
+    s, ctx = _on(dev, stream, (x, residual, gain, shift, out, None if at is None else seed))
+    with ctx:
+        if out is None:
+            h, ldh = torch.empty(x.shape, dtype=residual.dtype, device=dev), d
+        else:
+            h, (_, ldh) = out, _rows(out, "out", x.shape)
+            if h.device != dev or h.dtype != residual.dtype:
+                raise ValueError("out must be of residual's type and device")
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        stats = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+        _ok(lib().kf_dropout_norm(
+            s, KF_NORM_RMS if rms else KF_NORM_LAYER, _type(h.dtype, "residual"), _type(x.dtype, "x"),
+            rows, d, x.data_ptr(), ldx, residual.data_ptr(), ldres, p, host, at, site, _ptr(gain),
+            _ptr(shift), eps, h.data_ptr(), ldh, y.data_ptr(), d, stats.data_ptr()))
+    return h, y, stats
+
+
+def dropout_norm_backward(dy, h, gain, stats, p: float = 0.0, seed=0, site: int = 0,
+                          rms: bool = False, dres=None, stream=None):
+    """Gradients of dropout_norm (kf_dropout_norm_backward) from dy, that of y, and dres (like h;
+    None: none), that of h along the residual path: (dh, dx, dgain, dshift), dh like h and also the
+    gradient of residual, dx like dy, dgain and dshift [d] fp32, dshift None with rms."""
+    import torch
+    rows, ldh = _rows(h, "h")
+    _, lddy = _rows(dy, "dy", h.shape)
+    d, dev = h.shape[-1], h.device
+    lddres = d
+    if dres is not None:
+        _, lddres = _rows(dres, "dres", h.shape)
+        if dres.dtype != h.dtype or dres.device != dev:
+            raise ValueError("dres must be of h's type and device")
+    if dy.device != dev:
+        raise ValueError("dy must be on h's device")
+    _check(gain, "gain", dev, torch.float32, d)
+    _check(stats, "stats", dev, torch.float32, 2 * rows)
+    host, at = _seed(seed, dev)
+    s, ctx = _on(dev, stream, (dy, h, gain, stats, dres, None if at is None else seed))
+    with ctx:
+        dh = torch.empty(h.shape, dtype=h.dtype, device=dev)
+        dx = torch.empty(h.shape, dtype=dy.dtype, device=dev)
+        dgain = torch.empty(d, dtype=torch.float32, device=dev)
+        dshift = None if rms else torch.empty(d, dtype=torch.float32, device=dev)
+        n = lib().kf_layer_norm_backward_bytes(rows, d)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        _ok(lib().kf_dropout_norm_backward(
+            s, KF_NORM_RMS if rms else KF_NORM_LAYER, _type(h.dtype, "h"), _type(dy.dtype, "dy"), rows,
+            d, dy.data_ptr(), lddy, h.data_ptr(), ldh, _ptr(gain), stats.data_ptr(), _ptr(dres), lddres,
+            p, host, at, site, dh.data_ptr(), d, dx.data_ptr(), d, dgain.data_ptr(), _ptr(dshift),
+            ws.data_ptr(), n))
+    return dh, dx, dgain, dshift
+
+
+class PolicyLoss(NamedTuple):
+    loss: "torch.Tensor"
+    row_loss: "torch.Tensor"
+    logp: "torch.Tensor"
+    ratio: "torch.Tensor"
+    entropy: "torch.Tensor"
+    kl: "Optional[torch.Tensor]" = None
+    d_logits: "Optional[torch.Tensor]" = None
+
+
+def policy_loss(logits, tokens, advantages, old_logp=None, ref_logp=None, weights=None,
+                clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                entropy_coef: float = 0.0, grad: bool = True, out=None, stream=None) -> PolicyLoss:
+    """The clipped policy loss of tokens [...] int32 sampled from softmax(logits [..., vocab]), with
+    a KL term against ref_logp and an entropy bonus, and with grad its gradient d_logits
+    (kf_policy_loss).
+
+    advantages, old_logp (None: on policy), ref_logp (None: no KL term), weights (None: ones)
+    [...] fp32.  The ratio is clipped to [1 - clip_low, 1 + clip_high].  loss, 0-dimensional, is
+    the sum of row_loss, which has the weights in it: give weights of 1 / tokens for a mean.  A
+    row with a negative token or of weight 0 counts nothing: its results are 0.  out: where d_logits goes, logits itself if
+    they are not needed again.  No autograd graph."""
+    import torch
+    rows, ld = _rows(logits, "logits")
+    lead, V, dev = logits.shape[:-1], logits.shape[-1], logits.device
+    if tokens is None or advantages is None:
+        raise ValueError("tokens and advantages must be given")
+    _check(tokens, "tokens", dev, torch.int32, rows)
+    for t, n in ((advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights")):
+        _check(t, n, dev, torch.float32, rows)
+    if out is not None and not grad:
+        raise ValueError("out is where the gradient goes")
+    s, ctx = _on(dev, stream, (logits, tokens, advantages, old_logp, ref_logp, weights, out))
+    with ctx:
+        d, ldd = None, V
+        if out is not None:
+            d, (_, ldd) = out, _rows(out, "out", logits.shape)
+            if d.dtype != logits.dtype or d.device != dev:
+                raise ValueError("out must be of logits' type and device")
+        elif grad:
+            d = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        loss = torch.empty((), dtype=torch.float32, device=dev)
+        r = torch.empty((4 if ref_logp is None else 5, *lead), dtype=torch.float32, device=dev).unbind(0)
+        kl = r[4] if ref_logp is not None else None
+        _ok(lib().kf_policy_loss(
+            s, _type(logits.dtype, "logits"), rows, V, logits.data_ptr(), ld, _ptr(tokens),
+            _ptr(advantages), _ptr(old_logp), _ptr(ref_logp), _ptr(weights), 1.0 - clip_low,
+            1.0 + clip_high, kl_coef, entropy_coef, r[0].data_ptr(), r[1].data_ptr(), r[2].data_ptr(),
+            _ptr(kl), r[3].data_ptr(), loss.data_ptr(), _ptr(d), ldd))
+    return PolicyLoss(loss, *r[:4], kl, d)
 
 
 class GradClip:

@@ -16,9 +16,10 @@ OUT = os.path.join(PKG, "libkforcing.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["kf_api.cpp", "kf_train_api.cpp", "kf_kernels.hip", "kf_gemm.hip", "kf_blockattn.hip",
-           "kf_attnbwd.hip", "kf_norm.hip", "kf_logprobs.hip", "kf_clip.hip"]
+           "kf_attnbwd.hip", "kf_norm.hip", "kf_logprobs.hip", "kf_clip.hip", "kf_heads.hip",
+           "kf_dropout.hip", "kf_dropnorm.hip", "kf_policy.hip"]
 HEADERS = ["kf_internal.h", "kf_lds.h", "kf_attn.h", "kf_route.h", "kf_blockattn.h", "kf_rows.h",
-           "kf_train.h"]
+           "kf_train.h", "kf_norm.h", "kf_dropout.h", "kf_logprobs.h"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

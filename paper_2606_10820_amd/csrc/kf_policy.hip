@@ -1,0 +1,42 @@
+// kf_policy.hip -- the clipped policy loss of sampled tokens with a KL term and an entropy
+// bonus, from rows of logits, and its gradient.  With lp = l_t - lse, rho = exp(lp - old) and
+// d = ref - lp, a row's loss is
+//   L = -min(rho A, clip(rho) A) + beta (e^d - d - 1) - c H
+// (the KL term is the estimate of KL(policy | reference) from one sample that is never
+// negative and has the least variance), and with
+//   u = dL/dlp = -rho A [rho A <= clip(rho) A] - beta (e^d - 1)
+// the gradient of its logits is w (u ([v = t] - p_v) + c p_v (log p_v + H)).
+//
+// Bound by memory: the kernel of the token log probabilities (kf_logprobs.h) with the row's
+// gradients formed from its own logp and entropy, so the logits are read once; a loss formed
+// from log probabilities and sent back through them reads them twice.
+#include "kf_logprobs.h"
+
+namespace kf {
+namespace {
+
+// The rows' losses in fp64, in a fixed order.
+__global__ void __launch_bounds__(1024) policy_sum_kernel(const float* __restrict__ row_loss, int64_t rows, float* loss) {
+  __shared__ double part[16];
+  double v = 0;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < rows; i += 1024) v += (double)row_loss[i];
+  v = block_add<16>(v, part);
+  if (threadIdx.x == 0) *loss = (float)v;
+}
+
+}  // namespace
+
+hipError_t launch_policy_loss(const PolicyArgs& a, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.rows)
+    e = by_type(a.dtype, [&](auto t) {
+      using T = decltype(t);
+      return a.d_logits ? launch_by_width<T, true>(a, s) : launch_by_width<T, false>(a, s);
+    });
+  if (e != hipSuccess || !a.loss) return e;
+  launch(policy_sum_kernel, dim3(1), dim3(1024), 0, s, (const float*)a.row_loss, a.rows, a.loss);
+  return hipGetLastError();
+}
+
+}  // namespace kf

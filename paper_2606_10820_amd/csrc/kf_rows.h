@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include "kf_internal.h"
+#include "kforcing.h"
 
 namespace kf {
 
@@ -138,6 +139,28 @@ __device__ __forceinline__ S block_add(S v, S* part) {
     __syncthreads();
   }
   return v;
+}
+
+// f(X{}, Y{}) for elements of types x and y: equal ones, or x fp32 (a residual stream).
+template <typename F>
+inline hipError_t by_types(int x, int y, F&& f) {
+  if (x == KF_FP32 && y == KF_FP32) return f(float{}, float{});
+  if (x == KF_FP32 && y == KF_BF16) return f(float{}, bf16{});
+  if (x == KF_FP32 && y == KF_FP16) return f(float{}, f16{});
+  if (x == KF_BF16 && y == KF_BF16) return f(bf16{}, bf16{});
+  if (x == KF_FP16 && y == KF_FP16) return f(f16{}, f16{});
+  return hipErrorInvalidValue;
+}
+// The same, and x of 16 bits beside y fp32.
+template <typename F>
+inline hipError_t by_types_widening(int x, int y, F&& f) {
+  if (x == KF_BF16 && y == KF_FP32) return f(bf16{}, float{});
+  if (x == KF_FP16 && y == KF_FP32) return f(f16{}, float{});
+  return by_types(x, y, f);
+}
+// Whether rows at p, ld elements apart, take vectors of `bytes` bytes.
+inline bool vector_rows(const void* p, int64_t ld, int size, int bytes) {
+  return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) % bytes == 0;
 }
 
 }  // namespace kf

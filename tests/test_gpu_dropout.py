@@ -1,0 +1,214 @@
+"""GPU parity of dropout, its gradient, and dropout with a residual and a norm, against the
+generator in numpy and 64-bit references (bounds: tests/step_ref.py)."""
+import pytest
+
+from tests import step_ref as S
+from tests import train_ref as R
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+F32, BF, HF = torch.float32, torch.bfloat16, torch.float16
+KINDS = [(F32, F32), (BF, F32), (HF, F32), (BF, BF), (HF, HF), (F32, BF), (F32, HF)]
+PAIRS = [(F32, F32), (F32, BF), (F32, HF), (BF, BF), (HF, HF)]
+IDS = lambda v: str(v).replace("torch.", "")
+SEED = 0x9E3779B97F4A7C15
+
+
+@pytest.fixture(scope="module")
+def Bd():
+    from paper_2606_10820_amd import binding
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return binding
+
+
+def _inputs(rows, d, xt, yt, seed=0):
+    g = torch.Generator().manual_seed(seed + 13 * rows + d)
+    rnd = lambda *s: torch.randn(*s, generator=g)
+    return rnd(rows, d).to(xt), (3 * rnd(rows, d)).to(yt)
+
+
+SIZES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (1, 16), (7, 63), (9, 64), (3, 100), (33, 128), (5, 771), (11, 768), (3, 4099), (2, 8192), (1, 20001)]
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda p: f"{IDS(p[0])}-{IDS(p[1])}")
+@pytest.mark.parametrize("rows,d", SIZES)
+def test_parity(Bd, rows, d, kind):
+    x, res = _inputs(rows, d, *kind)
+    for p, site in ((0.1, 0), (0.5, 2 ** 31 - 1), (0.0, 3), (1.0, 3), (0.999, 5)):
+        for r in (None, res):
+            y = Bd.dropout(x.cuda(), p, SEED + rows, site, None if r is None else r.cuda(), kind[1])
+            ref, b = S.dropout(x, p, SEED + rows, site, r, kind[1])
+            assert R.worst(y, ref, b + 1e-300) <= 1, (p, r is None)
+        assert kind[1] == res.dtype
+    dx = Bd.dropout_backward(res.cuda(), 0.3, SEED, 7, kind[0])
+    ref, b = S.dropout(res, 0.3, SEED, 7, None, kind[0])
+    assert dx.dtype == kind[0] and R.worst(dx, ref, b + 1e-300) <= 1
+
+
+def test_share_kept_and_scale(Bd):
+    """Of 2^23 elements the kept ones are a binomial number: within six standard deviations; the mean of
+    kept ones is kept.  p goes to the nearest 1/65536."""
+    x = torch.ones(2048, 4096, device="cuda")
+    for p in (0.1, 0.5, 0.9):
+        y = Bd.dropout(x, p, 11, 1)
+        T = S.threshold(p)
+        q, n = 1 - T / 65536, x.numel()
+        k = int((y != 0).sum())
+        assert abs(k - q * n) <= 6 * (n * q * (1 - q)) ** 0.5
+        assert abs(float(y.max()) - 1 / q) <= 1e-6 / q
+    # seeds and sites are streams of their own: masks of two agree as often as chance has it
+    a = Bd.dropout(x, 0.5, 11, 1) != 0
+    for seed, site in ((12, 1), (11, 2), (11 + 2 ** 32, 1), (-11, 1)):
+        b = Bd.dropout(x, 0.5, seed, site) != 0
+        assert abs(int((a == b).sum()) - x.numel() / 2) <= 3 * x.numel() ** 0.5
+
+
+def test_dropped_elements_count_nothing(Bd):
+    """Infinities and NaN where the mask drops leave the residual as it is."""
+    x, res = _inputs(40, 256, BF, F32)
+    keep = S.kept(40, 256, 0.4, 5, 9)
+    x = torch.where(keep, x.float(), float("inf")).to(BF)
+    x[0][~keep[0]] = float("nan")
+    y = Bd.dropout(x.cuda(), 0.4, 5, 9, res.cuda()).cpu()
+    assert torch.equal(y[~keep], res[~keep]) and torch.isfinite(y).all()
+    assert not Bd.dropout(x.cuda(), 0.4, 5, 9).cpu()[~keep].any()
+
+
+@pytest.mark.parametrize("off,ld", [(0, 24), (1, 0), (3, 3), (4, 8), (2, 5)])
+@pytest.mark.parametrize("kind", KINDS[:4], ids=lambda p: f"{IDS(p[0])}-{IDS(p[1])}")
+def test_strides_and_in_place(Bd, kind, off, ld):
+    rows, d = 13, 104
+    x, res = _inputs(rows, d, *kind)
+
+    def strided(t, fill):
+        buf = torch.full((off + rows * (d + ld),), fill, dtype=t.dtype, device="cuda")
+        v = buf[off:].view(rows, d + ld)[:, :d]
+        v.copy_(t)
+        return buf, v
+    nan = float("nan")
+    want = Bd.dropout(x.cuda(), 0.2, 77, 4, res.cuda())
+    _, X = strided(x, nan)
+    rbuf, Rs = strided(res, 7.0)
+    got = Bd.dropout(X, 0.2, 77, 4, strided(res, nan)[1])
+    assert torch.equal(got, want)
+    y = Bd.dropout(X, 0.2, 77, 4, Rs, out=Rs)  # into the residual
+    assert y is Rs and torch.equal(Rs, want)
+    Rs.fill_(7.0)
+    assert (rbuf == 7).all()
+    if kind[0] == kind[1]:
+        plain = Bd.dropout(x.cuda(), 0.2, 77, 4)
+        assert torch.equal(Bd.dropout(X, 0.2, 77, 4, out=X), plain) and torch.equal(X, plain)
+
+
+def test_shapes_and_empty(Bd):
+    x, _ = _inputs(24, 40, F32, F32)
+    a = Bd.dropout(x.cuda(), 0.3, 3)
+    assert torch.equal(Bd.dropout(x.view(2, 3, 4, 40).cuda(), 0.3, 3).view(24, 40), a)
+    assert torch.equal(Bd.dropout(x[0].cuda(), 0.3, 3), a[0])
+    assert Bd.dropout(torch.zeros(0, 40, device="cuda"), 0.3, 3).shape == (0, 40)
+
+
+def test_past_32_bits(Bd):
+    """Elements past 2^31 and rows past 2^32."""
+    rows, d = 270_000, 8192
+    x = torch.ones(rows, d, dtype=BF, device="cuda")
+    Bd.dropout(x, 0.25, 21, 2, out=x)
+    assert torch.equal(x[-3:].cpu() != 0, S.kept(3, d, 0.25, 21, 2, rows - 3))
+    del x
+    rows = 2 ** 32 + 5
+    x = torch.ones(rows, 1, dtype=BF, device="cuda")
+    Bd.dropout(x, 0.25, 21, 2, out=x)
+    for r in (0, 2 ** 31 - 2, 2 ** 32 - 3, rows - 5):
+        assert torch.equal(x[r:r + 5].cpu() != 0, S.kept(5, 1, 0.25, 21, 2, r))
+
+
+def test_seed_on_the_device(Bd):
+    """A seed in device memory is the same number; a captured call draws by what it holds at each
+    replay."""
+    x = torch.randn(300, 96, device="cuda")
+    for v in (0, 5, -3, 2 ** 62):
+        s = torch.tensor([v], device="cuda")
+        assert torch.equal(Bd.dropout(x, 0.3, s, 6), Bd.dropout(x, 0.3, v, 6))
+    s = torch.tensor([1], device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        Bd.dropout(x, 0.3, s, 6)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = Bd.dropout(x, 0.3, s, 6)
+        s.add_(1)
+    for v in (1, 2, 3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, Bd.dropout(x, 0.3, v, 6)), v
+
+
+# ------------------------------------------------ with a residual and a norm
+@pytest.mark.parametrize("rms", [False, True], ids=["layer", "rms"])
+@pytest.mark.parametrize("pair", PAIRS, ids=lambda p: f"{IDS(p[0])}-{IDS(p[1])}")
+@pytest.mark.parametrize("rows,d", [(1, 1), (3, 2), (2, 8), (5, 63), (1, 64), (7, 100), (33, 128), (9, 256), (13, 257), (6, 512), (10, 520), (131, 768), (12, 771),
+                                    (65, 1024), (9, 1028), (4, 1536), (5, 2048), (3, 2049), (4, 4096), (3, 5000), (2, 8192), (2, 8200), (2, 20001)])
+def test_norm_is_dropout_then_norm(Bd, rows, d, pair, rms):
+    """Bit for bit the two operators one after the other, both ways (each is held to its reference)."""
+    ht, yt = pair
+    x, res = (t.cuda() for t in _inputs(rows, d, yt, ht))
+    dy, dres = (t.cuda() for t in _inputs(rows, d, yt, ht, seed=5))
+    g = torch.Generator().manual_seed(d)
+    gain, shift = (1 + 0.2 * torch.randn(d, generator=g)).cuda(), None if rms else torch.randn(d, generator=g).cuda()
+    for p, site in ((0.1, 3), (0.0, 0), (1.0, 1)):
+        h0 = Bd.dropout(x, p, SEED, site, res)
+        y0, st0 = Bd.layer_norm(h0, gain, shift, rms=rms, out_dtype=yt)
+        h, y, st = Bd.dropout_norm(x, res, gain, shift, p, SEED, site, rms=rms)
+        assert torch.equal(h, h0) and torch.equal(y, y0) and torch.equal(st, st0)
+        for r in (dres, None):
+            dh0, dg0, db0 = Bd.layer_norm_backward(dy, h0, gain, st0, rms, r)
+            dx0 = Bd.dropout_backward(dh0, p, SEED, site, yt)
+            dh, dx, dg, db = Bd.dropout_norm_backward(dy, h, gain, st, p, SEED, site, rms, r)
+            assert torch.equal(dh, dh0) and torch.equal(dx, dx0) and torch.equal(dg, dg0)
+            assert db is None and rms or torch.equal(db, db0)
+
+
+@pytest.mark.parametrize("rows", [0, 1, 31, 32, 33, 2047, 50_001])
+def test_norm_rows(Bd, rows):
+    for d, (ht, yt) in ((40, PAIRS[1]), (96, PAIRS[3]), (33, PAIRS[0])):
+        x, res = (t.cuda() for t in _inputs(rows, d, yt, ht))
+        gain, shift = torch.ones(d, device="cuda"), torch.zeros(d, device="cuda")
+        h, y, st = Bd.dropout_norm(x, res, gain, shift, 0.3, 8, 1)
+        dh, dx, dg, db = Bd.dropout_norm_backward(y, h, gain, st, 0.3, 8, 1)
+        h0 = Bd.dropout(x, 0.3, 8, 1, res)
+        y0, st0 = Bd.layer_norm(h0, gain, shift, out_dtype=yt)
+        dh0, dg0, db0 = Bd.layer_norm_backward(y0, h0, gain, st0)
+        want = (h0, y0, dh0, Bd.dropout_backward(dh0, 0.3, 8, 1, yt), dg0, db0)
+        assert all(torch.equal(a, b) for a, b in zip((h, y, dh, dx, dg, db), want))
+
+
+@pytest.mark.parametrize("off,ld", [(0, 32), (1, 0), (3, 3), (4, 4)])
+@pytest.mark.parametrize("pair", [PAIRS[1], PAIRS[3]], ids=["fp32-bf16", "bf16-bf16"])
+def test_norm_strides_and_in_place(Bd, pair, off, ld):
+    ht, yt = pair
+    rows, d = 11, 768
+    x, res = _inputs(rows, d, yt, ht)
+    dy, dres = _inputs(rows, d, yt, ht, seed=9)
+
+    def strided(t, fill=float("nan")):
+        buf = torch.full((off + rows * (d + ld),), fill, dtype=t.dtype, device="cuda")
+        v = buf[off:].view(rows, d + ld)[:, :d]
+        v.copy_(t)
+        return buf, v
+    gain = torch.full((d,), 0.7, device="cuda")
+    h0 = strided(torch.zeros_like(res))[1]
+    Bd.dropout(x.cuda(), 0.2, 5, 6, res.cuda(), out=h0)
+    y0, st0 = Bd.layer_norm(h0, gain, out_dtype=yt)
+    X, (rbuf, Rs) = strided(x)[1], strided(res, 7.0)
+    h, y, st = Bd.dropout_norm(X, Rs, gain, None, 0.2, 5, 6, out=Rs)  # the stream in place
+    assert h is Rs and all(torch.equal(a, b) for a, b in zip((h, y, st), (h0, y0, st0)))
+    DY, DR = strided(dy)[1], strided(dres)[1]
+    dh0, dg0, db0 = Bd.layer_norm_backward(DY, h0, gain, st0, dres=DR)
+    dh, dx, dg, db = Bd.dropout_norm_backward(DY, h, gain, st, 0.2, 5, 6, dres=DR)
+    want = (dh0, Bd.dropout_backward(dh0, 0.2, 5, 6, yt), dg0, db0)
+    assert all(torch.equal(a, b) for a, b in zip((dh, dx, dg, db), want))
+    Rs.fill_(7.0)
+    assert (rbuf == 7).all()
