@@ -17,22 +17,35 @@ namespace kf {
 namespace {
 
 // A head is held by G lanes, a power of two, eight columns each (a pair never leaves its
-// lane); a wavefront takes 64 / G heads of one token at a time and kAhead such rounds of it
-// with all their loads in flight, so that a token's turns are loaded once.
-constexpr int kHeadThreads = 256, kAhead = 6;
+// lane): eight in a row where rows are whole vectors of 16 bytes, else four pairs G apart.  A workgroup's heads are of one kind, so that what a kind needs is uniform; a
+// wavefront takes `side` heads (the largest power of two that divides their number, at most
+// 64 / G) of 64 / G / side consecutive tokens at a time, every lane with work, and up to kAhead
+// rounds of further heads of the same tokens with all their loads in flight and their turns
+// loaded once.
+constexpr int kHeadThreads = 256, kHeadWaves = kHeadThreads / 64, kAhead = 4;
 
-// Sum over aligned groups of G lanes, the same in every lane.
-__device__ __forceinline__ float group_add(float v, int G) {
-  if (G > 1) v += dpp<0xB1>(v);   // lane ^ 1
-  if (G > 2) v += dpp<0x4E>(v);   // lane ^ 2
-  if (G > 4) v += dpp<0x141>(v);  // 7 - lane: the other four of eight, equal by now
-  if (G > 8) v += dpp<0x140>(v);  // 15 - lane
-  if (G > 16) {
+// The heads of one kind (0 queries, 1 keys, 2 values): `rounds` of them a chunk.
+struct HeadsKind {
+  int heads, first, side_log, rounds, chunks;
+};
+struct HeadsSplit {
+  HeadsKind kind[3];
+  int G_log, l_log;
+  uint32_t l_inv;  // t / L = t l_inv >> 30 + l_log for t up to 2^30
+};
+
+// Sum over aligned groups of 2^n lanes, the same in every lane.
+__device__ __forceinline__ float group_add(float v, int n) {
+  if (n > 0) v += dpp<0xB1>(v);   // lane ^ 1
+  if (n > 1) v += dpp<0x4E>(v);   // lane ^ 2
+  if (n > 2) v += dpp<0x141>(v);  // 7 - lane: the other four of eight, equal by now
+  if (n > 3) v += dpp<0x140>(v);  // 15 - lane
+  if (n > 4) {
     const unsigned u = __float_as_uint(v);
     const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
   }
-  if (G > 32) {
+  if (n > 5) {
     const unsigned u = __float_as_uint(v);
     const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
@@ -40,41 +53,71 @@ __device__ __forceinline__ float group_add(float v, int G) {
   return v;
 }
 
-// Eight columns from `col` of a row of dh; VEC: the row is whole vectors of eight.
-template <bool VEC, typename T>
-__device__ __forceinline__ void load8(const T* p, int left, float (&f)[8]) {
-  if constexpr (VEC) {
-    load_f<8>(p, f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = j < left ? (float)p[j] : 0.f;
-  }
-}
-template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T* p, int left, const float (&f)[8]) {
-  if constexpr (VEC) {
-    store_f<8>(p, f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < left) p[j] = (T)f[j];
-  }
+// 1 / sqrt(v), of one rounding or so also where v is below the normal numbers (eps 0).
+__device__ __forceinline__ float root(float v) {
+  const bool tiny = v < 0x1p-100f;
+  return __builtin_amdgcn_rsqf(tiny ? v * 0x1p100f : v) * (tiny ? 0x1p50f : 1.0f);
 }
 
-// cos and sin of the lane's four pairs for a token, the first n of them turned; a position
+// The columns of lane c of G.  E: elements an access takes, 8 (in pieces of 16 bytes), 2 or 1.
+template <int E>
+struct HeadCols {
+  int c, G, dh;
+  __device__ __forceinline__ int pair(int i) const { return E == 8 ? c * 4 + i : c + G * i; }
+  __device__ __forceinline__ int at(int j) const { return 2 * pair(j / 2) + (j & 1); }
+  __device__ __forceinline__ bool any() const { return (E == 8 ? c * 8 : 2 * c) < dh; }
+  template <typename T>
+  __device__ __forceinline__ void load(const T* p, float (&f)[8]) const {
+    if constexpr (E == 8) {
+      load_f<8>(p + c * 8, f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[2] = {0.f, 0.f};
+        if constexpr (E == 2) {
+          if (2 * pair(i) < dh) load_f<2>(p + 2 * pair(i), v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            if (2 * pair(i) + k < dh) v[k] = (float)p[2 * pair(i) + k];
+        }
+        f[2 * i] = v[0];
+        f[2 * i + 1] = v[1];
+      }
+    }
+  }
+  // Past the caches: results are read by other kernels, after all of them are written.
+  template <typename T>
+  __device__ __forceinline__ void store(T* p, const float (&f)[8]) const {
+    constexpr int P = E == 8 ? 16 / sizeof(T) : E;
+#pragma unroll
+    for (int k = 0; k < 8; k += P) {
+      float v[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[i] = f[k + i];
+      if constexpr (E == 8) {
+        stream_out<P>(p + at(0) + k, v);
+      } else {
+        if (at(k) < dh) store_f<P>(p + at(k), v);
+      }
+    }
+  }
+};
+
+// cos and sin of the lane's four pairs for a token, and which of them are turned; a position
 // outside the table: NaN.
 struct Turn {
   float c[4], s[4];
-  int n;
-  __device__ __forceinline__ void load(const HeadsArgs& a, int b, int l, int col) {
-    n = (a.d_rot - col) / 2;
-    if (!a.d_rot) return;
+  bool on[4] = {false, false, false, false};
+  template <int E>
+  __device__ __forceinline__ void load(const HeadsArgs& a, int b, int l, const HeadCols<E>& cols) {
     const int p = a.pos ? a.pos[b * a.pos_ld + l] : l;
     const bool in = p >= 0 && p < a.n_pos;
     const float2* row = a.table + (int64_t)(in ? p : 0) * (a.d_rot / 2);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 t = row[i < n ? col / 2 + i : 0];
+      on[i] = cols.pair(i) < a.d_rot / 2;
+      const float2 t = row[on[i] ? cols.pair(i) : 0];
       c[i] = in ? t.x : NAN;
       s[i] = in ? t.y : NAN;
     }
@@ -83,167 +126,186 @@ struct Turn {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float x = f[2 * i], y = f[2 * i + 1], t = way * s[i];
-      f[2 * i] = i < n ? x * c[i] - y * t : x;
-      f[2 * i + 1] = i < n ? x * t + y * c[i] : y;
+      f[2 * i] = on[i] ? x * c[i] - y * t : x;
+      f[2 * i + 1] = on[i] ? x * t + y * c[i] : y;
     }
   }
 };
 
-template <typename X, typename Y, bool VEC, bool NORM>
-__global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, int G, int rounds) {
-  const int lane = threadIdx.x & 63, col = lane % G * 8, left = a.dh - col, per = 64 / G;
-  const bool on = left > 0;
-  const int Hqk = a.Hq + a.Hkv, H = Hqk + a.Hkv, tokens = a.B * a.L;
-  const int h0 = blockIdx.y * rounds * per + lane / G;
-  const float inv = 1.0f / (float)a.dh;
-  float gq[8], gk[8];
-  if constexpr (NORM) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      gq[j] = a.gq && j < left ? a.gq[col + j] : 1.f;
-      gk[j] = a.gk && j < left ? a.gk[col + j] : 1.f;
+// This thread's part of a launch.
+struct HeadsAt {
+  int kind, round0, rounds, side_log, sub, first, l_tokens;
+  HeadsView view;
+  const float* gain;
+  __device__ __forceinline__ HeadsAt(const HeadsArgs& a, const HeadsSplit& s) {
+    int chunk = blockIdx.y;
+    kind = 0;
+    if (chunk >= s.kind[0].chunks) {
+      chunk -= s.kind[0].chunks;
+      kind = 1;
+      if (chunk >= s.kind[1].chunks) {
+        chunk -= s.kind[1].chunks;
+        kind = 2;
+      }
     }
+    const HeadsKind& k = s.kind[kind];
+    side_log = k.side_log;
+    const int all = k.heads >> side_log;
+    round0 = chunk * k.rounds;
+    rounds = min(k.rounds, all - round0);
+    first = k.first;
+    view = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+    gain = kind == 0 ? a.gq : kind == 1 ? a.gk : nullptr;
+    const int lane = threadIdx.x & 63;
+    sub = lane >> s.G_log;
+    l_tokens = 6 - s.G_log - side_log;  // log2 of a wavefront's tokens
   }
-  for (int t = blockIdx.x * (kHeadThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); t < tokens;
-       t += gridDim.x * (kHeadThreads / 64)) {
-    const int b = t / a.L, l = t - b * a.L;
-    const X* x = static_cast<const X*>(a.x) + (int64_t)t * a.ldx + col;
+};
+
+template <typename X, typename Y, int E>
+__global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, HeadsSplit s) {
+  const HeadsAt at(a, s);
+  if (!at.view.p) return;
+  const HeadCols<E> cols{(int)(threadIdx.x & ((1 << s.G_log) - 1)), 1 << s.G_log, a.dh};
+  const bool norm = at.gain != nullptr, turned = at.kind < 2 && a.d_rot;
+  const int tokens = a.B * a.L, side = 1 << at.side_log, h0 = at.round0 * side + (at.sub & (side - 1));
+  const float inv = 1.0f / (float)a.dh;
+  float g[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) g[j] = norm && cols.at(j) < a.dh ? at.gain[cols.at(j)] : 1.f;
+  for (int t0 = (blockIdx.x * kHeadWaves + (threadIdx.x >> 6)) << at.l_tokens; t0 < tokens;
+       t0 += (gridDim.x * kHeadWaves) << at.l_tokens) {
+    const int t = t0 + (at.sub >> at.side_log);
+    const bool on = cols.any() && t < tokens;
+    const int b = (int)((uint64_t)t * s.l_inv >> (30 + s.l_log)), l = t - b * a.L;
+    const X* x = static_cast<const X*>(a.x) + (int64_t)t * a.ldx + (int64_t)(at.first + h0) * a.dh;
+    Y* y = static_cast<Y*>(at.view.p) + b * at.view.batch + h0 * at.view.head + l * at.view.row;
     float f[kAhead][8];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int h = h0 + i * per;
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[i][j] = 0.f;
-      if (i < rounds && on && h < H) load8<VEC>(x + (int64_t)h * a.dh, left, f[i]);
+      if (i < at.rounds && on) cols.load(x + i * side * a.dh, f[i]);
     }
     Turn turn;
-    turn.load(a, b, l, col);
+    if (turned && on) turn.load(a, b, l, cols);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int h = h0 + i * per;
-      if (i >= rounds) break;
-      const bool isq = h < a.Hq, isk = h < Hqk;
-      if constexpr (NORM) {
+      if (i >= at.rounds) break;
+      if (norm) {
         float q = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) q += f[i][j] * f[i][j];
-        const float r = 1.0f / sqrtf(group_add(q, G) * inv + a.eps);
-        const bool normed = isq ? a.gq != nullptr : isk && a.gk != nullptr;
+        const float r = root(group_add(q, s.G_log) * inv + a.eps);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[i][j] = normed ? f[i][j] * r * (isq ? gq[j] : gk[j]) : f[i][j];
+        for (int j = 0; j < 8; ++j) f[i][j] = f[i][j] * r * g[j];
       }
-      if (isk && a.d_rot) turn.turn(f[i], 1.f);
-      const HeadsView& o = isq ? a.q : isk ? a.k : a.v;
-      const int ho = isq ? h : isk ? h - a.Hq : h - Hqk;
-      if (on && h < H && o.p)
-        store8<VEC>(static_cast<Y*>(o.p) + b * o.batch + ho * o.head + l * o.row + col, left, f[i]);
+      if (turned) turn.turn(f[i], 1.f);
+      if (on) cols.store(y + i * (side * at.view.head), f[i]);
     }
   }
 }
 
 // Gains' gradients are summed in registers, a lane's eight columns over its tokens and heads,
-// then over a workgroup's lanes of the same columns, and leave as [2][dh] of the strip.
-template <typename X, typename Y, bool VEC, bool NORM>
-__global__ void __launch_bounds__(kHeadThreads) heads_grad_kernel(HeadsArgs a, int G, int rounds, float* part) {
-  constexpr int NW = kHeadThreads / 64;
-  const int lane = threadIdx.x & 63, col = lane % G * 8, left = a.dh - col, per = 64 / G;
-  const bool on = left > 0;
-  const int Hqk = a.Hq + a.Hkv, H = Hqk + a.Hkv, tokens = a.B * a.L;
-  const int h0 = blockIdx.y * rounds * per + lane / G;
+// then over a workgroup's lanes of the same columns, and leave as [dh] of the strip.
+template <typename X, typename Y, int E>
+__global__ void __launch_bounds__(kHeadThreads) heads_grad_kernel(HeadsArgs a, HeadsSplit s, float* part) {
+  __shared__ float sums[kHeadWaves][512];
+  const HeadsAt at(a, s);
+  const HeadCols<E> cols{(int)(threadIdx.x & ((1 << s.G_log) - 1)), 1 << s.G_log, a.dh};
+  const bool norm = at.gain != nullptr, turned = at.kind < 2 && a.d_rot, given = at.view.p != nullptr;
+  const int tokens = a.B * a.L, side = 1 << at.side_log, h0 = at.round0 * side + (at.sub & (side - 1));
   const float inv = 1.0f / (float)a.dh;
-  constexpr int kDepth = NORM ? 3 : kAhead;
-  float gq[8], gk[8], aq[8], ak[8];
-  if constexpr (NORM) {
+  float g[8], sum[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      gq[j] = a.gq && j < left ? a.gq[col + j] : 1.f;
-      gk[j] = a.gk && j < left ? a.gk[col + j] : 1.f;
-      aq[j] = ak[j] = 0.f;
-    }
+  for (int j = 0; j < 8; ++j) {
+    g[j] = norm && cols.at(j) < a.dh ? at.gain[cols.at(j)] : 1.f;
+    sum[j] = 0.f;
   }
-  for (int t = blockIdx.x * NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); t < tokens; t += gridDim.x * NW) {
-    const int b = t / a.L, l = t - b * a.L;
-    const X* x = static_cast<const X*>(a.x) + (int64_t)t * a.ldx + col;
-    X* dx = static_cast<X*>(a.dx) + (int64_t)t * a.lddx + col;
+  for (int t0 = (blockIdx.x * kHeadWaves + (threadIdx.x >> 6)) << at.l_tokens; t0 < tokens;
+       t0 += (gridDim.x * kHeadWaves) << at.l_tokens) {
+    const int t = t0 + (at.sub >> at.side_log);
+    const bool on = cols.any() && t < tokens;
+    const int b = (int)((uint64_t)t * s.l_inv >> (30 + s.l_log)), l = t - b * a.L;
+    const int64_t xcol = (int64_t)(at.first + h0) * a.dh;
+    const X* x = static_cast<const X*>(a.x) + (int64_t)t * a.ldx + xcol;
+    X* dx = static_cast<X*>(a.dx) + (int64_t)t * a.lddx + xcol;
+    const Y* dy = static_cast<const Y*>(at.view.p) + b * at.view.batch + h0 * at.view.head + l * at.view.row;
+    float f[kAhead][8], w[kAhead][8];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = w[i][j] = 0.f;
+      if (i < at.rounds && on && given) {
+        cols.load(dy + i * (side * at.view.head), w[i]);
+        if (norm) cols.load(x + i * side * a.dh, f[i]);
+      }
+    }
     Turn turn;
-    turn.load(a, b, l, col);
-    for (int i0 = 0; i0 < rounds; i0 += kDepth) {
-      float f[kDepth][8], w[kDepth][8];
-      bool given[kDepth];
+    if (turned && on) turn.load(a, b, l, cols);
 #pragma unroll
-      for (int i = 0; i < kDepth; ++i) {
-        const int h = h0 + (i0 + i) * per;
-        const bool isq = h < a.Hq, isk = h < Hqk, here = i0 + i < rounds && on && h < H;
-        const HeadsView& o = isq ? a.q : isk ? a.k : a.v;
-        const int ho = isq ? h : isk ? h - a.Hq : h - Hqk;
-        given[i] = here && o.p;
+    for (int i = 0; i < kAhead; ++i) {
+      if (i >= at.rounds) break;
+      if (turned && given) turn.turn(w[i], -1.f);
+      if (norm && given) {
+        float q = 0.f, m = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[i][j] = w[i][j] = 0.f;
-        if (given[i]) {
-          load8<VEC>(static_cast<const Y*>(o.p) + b * o.batch + ho * o.head + l * o.row + col, left, w[i]);
-          if (NORM && (isq ? a.gq != nullptr : isk && a.gk != nullptr)) load8<VEC>(x + (int64_t)h * a.dh, left, f[i]);
+        for (int j = 0; j < 8; ++j) q += f[i][j] * f[i][j];
+        const float r = root(group_add(q, s.G_log) * inv + a.eps);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          f[i][j] *= r;
+          const float wx = on ? w[i][j] * f[i][j] : 0.f;
+          sum[j] += wx;
+          m += wx * g[j];
         }
+        m = group_add(m, s.G_log) * inv;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[i][j] = r * (w[i][j] * g[j] - f[i][j] * m);
       }
-#pragma unroll
-      for (int i = 0; i < kDepth; ++i) {
-        const int h = h0 + (i0 + i) * per;
-        if (i0 + i >= rounds) break;
-        const bool isq = h < a.Hq, isk = h < Hqk;
-        if (isk && a.d_rot && given[i]) turn.turn(w[i], -1.f);
-        if constexpr (NORM) {
-          const bool normed = isq ? a.gq != nullptr : isk && a.gk != nullptr;
-          float q = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) q += f[i][j] * f[i][j];
-          const float r = 1.0f / sqrtf(group_add(q, G) * inv + a.eps);
-          float m = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            f[i][j] *= r;
-            const float wx = w[i][j] * f[i][j];
-            if (normed) {
-              aq[j] += isq ? wx : 0.f;
-              ak[j] += isq ? 0.f : wx;
-            }
-            const float g = isq ? gq[j] : gk[j];
-            m += wx * g;
-            w[i][j] = normed ? w[i][j] * g : w[i][j];
-          }
-          m = group_add(m, G) * inv;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w[i][j] = normed ? r * (w[i][j] - f[i][j] * m) : w[i][j];
-        }
-        if (on && h < H) store8<VEC>(dx + (int64_t)h * a.dh, left, w[i]);
-      }
+      if (on) cols.store(dx + i * side * a.dh, w[i]);
     }
   }
-  if constexpr (NORM) {
-    if (!part) return;
-    __shared__ float sums[NW][2][512];
-    for (int off = G; off < 64; off <<= 1) {
+  if (!part || !norm) return;
+  for (int off = 1 << s.G_log; off < 64; off <<= 1) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        aq[j] += __shfl_xor(aq[j], off, 64);
-        ak[j] += __shfl_xor(ak[j], off, 64);
-      }
-    }
-    if (lane < G) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sums[threadIdx.x >> 6][0][col + j] = aq[j];
-        sums[threadIdx.x >> 6][1][col + j] = ak[j];
-      }
-    }
-    __syncthreads();
-    float* to = part + (size_t)(blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.dh;
-    for (int i = threadIdx.x; i < 2 * a.dh; i += kHeadThreads) {
-      const int which = i >= a.dh, c = i - which * a.dh;
-      float v = sums[0][which][c];
-#pragma unroll
-      for (int k = 1; k < NW; ++k) v += sums[k][which][c];
-      to[i] = v;
-    }
+    for (int j = 0; j < 8; ++j) sum[j] += __shfl_xor(sum[j], off, 64);
   }
+  if (at.sub == 0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[threadIdx.x >> 6][cols.at(j)] = sum[j];
+  }
+  __syncthreads();
+  float* to = part + (size_t)(blockIdx.y * gridDim.x + blockIdx.x) * a.dh;
+  for (int i = threadIdx.x; i < a.dh; i += kHeadThreads) {
+    float v = sums[0][i];
+#pragma unroll
+    for (int k = 1; k < kHeadWaves; ++k) v += sums[k][i];
+    to[i] = v;
+  }
+}
+
+// The strips' sums joined, 32 columns of one gain (blockIdx.y) by 32 groups of strips; zeros
+// of no strips.
+__global__ void __launch_bounds__(1024) heads_gain_kernel(const float* __restrict__ part, int q_strips, int k_strips, int dh, float* dgq, float* dgk) {
+  __shared__ float sum[32][33];
+  const int c = threadIdx.x & 31, grp = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+  const bool keys = blockIdx.y;
+  float* to = keys ? dgk : dgq;
+  if (!to) return;
+  const int n = keys ? k_strips : q_strips;
+  const float* p = part + (keys ? (size_t)q_strips * dh : 0);
+  float v = 0.f;
+  if (col < dh) {
+#pragma unroll 8
+    for (int i = grp; i < n; i += 32) v += p[(size_t)i * dh + col];
+  }
+  sum[grp][c] = v;
+  __syncthreads();
+  if (grp || col >= dh) return;
+#pragma unroll
+  for (int i = 1; i < 32; ++i) v += sum[i][c];
+  to[col] = v;
 }
 
 __global__ void __launch_bounds__(256) rope_table_kernel(int64_t n, int pairs, double base, float2* table) {
@@ -257,23 +319,48 @@ __global__ void __launch_bounds__(256) rope_table_kernel(int64_t n, int pairs, d
   }
 }
 
-struct Split {
-  int G, rounds, parts;
-  explicit Split(const HeadsArgs& a) {
-    G = 1;
-    while (G * 8 < a.dh) G *= 2;
-    const int per = 64 / G, all = (a.Hq + 2 * a.Hkv + per - 1) / per;
-    parts = (all + kAhead - 1) / kAhead;
-    rounds = (all + parts - 1) / parts;
-    parts = (all + rounds - 1) / rounds;
+HeadsSplit split(const HeadsArgs& a) {
+  HeadsSplit s = {};
+  while ((8 << s.G_log) < a.dh) ++s.G_log;
+  while (((int64_t)1 << s.l_log) < a.L) ++s.l_log;
+  s.l_inv = (uint32_t)((((uint64_t)1 << (30 + s.l_log)) + a.L - 1) / a.L);
+  const int heads[3] = {a.Hq, a.Hkv, a.Hkv}, first[3] = {0, a.Hq, a.Hq + a.Hkv};
+  for (int i = 0; i < 3; ++i) {
+    HeadsKind& k = s.kind[i];
+    k.heads = heads[i];
+    k.first = first[i];
+    if (!k.heads) continue;
+    while (k.side_log < 5 - s.G_log && k.heads % (2 << k.side_log) == 0) ++k.side_log;
+    const int all = k.heads >> k.side_log;
+    k.chunks = (all + kAhead - 1) / kAhead;
+    k.rounds = (all + k.chunks - 1) / k.chunks;
+    k.chunks = (all + k.rounds - 1) / k.rounds;
   }
-};
-
-bool vector_view(const HeadsView& v, int size) {
-  return !v.p || (reinterpret_cast<uintptr_t>(v.p) | (uintptr_t)(v.batch * size) | (uintptr_t)(v.head * size) | (uintptr_t)(v.row * size)) % 16 == 0;
+  return s;
 }
-bool vector_heads(const HeadsArgs& a, int ys) {
-  return a.dh % 8 == 0 && vector_view(a.q, ys) && vector_view(a.k, ys) && vector_view(a.v, ys);
+int chunks(const HeadsSplit& s) { return s.kind[0].chunks + s.kind[1].chunks + s.kind[2].chunks; }
+// Workgroups for all tokens, each wavefront's once, by the kind that takes the fewest tokens
+// a wavefront.
+int64_t token_groups(const HeadsArgs& a, const HeadsSplit& s) {
+  int side = 0;
+  for (int i = 0; i < 3; ++i) side = std::max(side, s.kind[i].side_log);
+  const int64_t per = (int64_t)kHeadWaves << (6 - s.G_log - side);
+  return ((int64_t)a.B * a.L + per - 1) / per;
+}
+
+// Elements an access may take: of heads dh apart in rows ld apart, and of views.
+int row_elements(const void* p, int64_t ld, int dh, int size) {
+  if (dh % 8 == 0 && vector_rows(p, ld, size, 16)) return 8;
+  return dh % 2 == 0 && vector_rows(p, ld, size, 2 * size) ? 2 : 1;
+}
+int view_elements(const HeadsView& v, int dh, int size) {
+  if (!v.p) return 8;
+  const uintptr_t all = reinterpret_cast<uintptr_t>(v.p) | (uintptr_t)(v.batch * size) | (uintptr_t)(v.head * size) | (uintptr_t)(v.row * size);
+  if (dh % 8 == 0 && all % 16 == 0) return 8;
+  return dh % 2 == 0 && all % (2 * size) == 0 ? 2 : 1;
+}
+int views_elements(const HeadsArgs& a, int size) {
+  return std::min({view_elements(a.q, a.dh, size), view_elements(a.k, a.dh, size), view_elements(a.v, a.dh, size)});
 }
 
 }  // namespace
@@ -282,28 +369,26 @@ hipError_t launch_heads(const HeadsArgs& a, hipStream_t s) {
   return by_types(a.x_dtype, a.y_dtype, [&](auto xt, auto yt) {
     using X = decltype(xt);
     using Y = decltype(yt);
-    const Split sp(a);
-    const int64_t need = ((int64_t)a.B * a.L + kHeadThreads / 64 - 1) / (kHeadThreads / 64);
-    const int64_t most = std::max<int64_t>(1, (1 << 16) / sp.parts);
-    const dim3 grid((unsigned)(need < most ? need : most), (unsigned)sp.parts);
-    const bool vec = vector_heads(a, sizeof(Y)) && vector_rows(a.x, a.ldx, sizeof(X), 16);
-    auto go = [&](auto kernel) {
-      launch(kernel, grid, dim3(kHeadThreads), 0, s, a, sp.G, sp.rounds);
-      return hipGetLastError();
-    };
-    const bool norm = a.gq || a.gk;
-    if (vec) return norm ? go(heads_kernel<X, Y, true, true>) : go(heads_kernel<X, Y, true, false>);
-    return norm ? go(heads_kernel<X, Y, false, true>) : go(heads_kernel<X, Y, false, false>);
+    const HeadsSplit sp = split(a);
+    const int y = chunks(sp);
+    const dim3 grid((unsigned)std::min<int64_t>(token_groups(a, sp), std::max(1, (1 << 18) / y)), (unsigned)y);
+    const int e = std::min(views_elements(a, sizeof(Y)), row_elements(a.x, a.ldx, a.dh, sizeof(X)));
+    auto kernel = e == 8 ? heads_kernel<X, Y, 8> : e == 2 ? heads_kernel<X, Y, 2> : heads_kernel<X, Y, 1>;
+    launch(kernel, grid, dim3(kHeadThreads), 0, s, a, sp);
+    return hipGetLastError();
   });
 }
 
-// Workgroups with sums: enough to fill the chip (a wavefront's registers leave four a SIMD).
-constexpr int kHeadStrips = 1024;
+// Workgroups with sums, at most, over all chunks.
+constexpr int kHeadStrips = 2048;
+namespace {
+int grad_blocks(const HeadsArgs& a, const HeadsSplit& sp) {
+  return (int)std::min<int64_t>(token_groups(a, sp), std::max(1, kHeadStrips / chunks(sp)));
+}
+}  // namespace
 int heads_strips(const HeadsArgs& a) {
-  const Split sp(a);
-  const int64_t need = ((int64_t)a.B * a.L + kHeadThreads / 64 - 1) / (kHeadThreads / 64);
-  const int64_t most = std::max(1, kHeadStrips / sp.parts);
-  return (int)((need < most ? need : most) * sp.parts);
+  const HeadsSplit sp = split(a);
+  return grad_blocks(a, sp) * (sp.kind[0].chunks + sp.kind[1].chunks);
 }
 
 hipError_t launch_heads_grad(const HeadsArgs& a, float* dgq, float* dgk, float* part, hipStream_t s) {
@@ -311,24 +396,24 @@ hipError_t launch_heads_grad(const HeadsArgs& a, float* dgq, float* dgk, float* 
     using X = decltype(xt);
     using Y = decltype(yt);
     const bool norm = a.gq || a.gk, sums = dgq || dgk;
-    int strips = 0;
+    int strips[2] = {0, 0};
     if (a.B && a.L) {
-      const Split sp(a);
-      const int64_t need = ((int64_t)a.B * a.L + kHeadThreads / 64 - 1) / (kHeadThreads / 64);
-      strips = heads_strips(a);
-      const int64_t most = norm ? strips / sp.parts : std::max<int64_t>(1, (1 << 16) / sp.parts);
-      const dim3 grid((unsigned)(need < most ? need : most), (unsigned)sp.parts);
-      const bool vec = vector_heads(a, sizeof(Y)) && vector_rows(a.dx, a.lddx, sizeof(X), 16) &&
-                       (!norm || vector_rows(a.x, a.ldx, sizeof(X), 16));
-      auto go = [&](auto kernel) {
-        launch(kernel, grid, dim3(kHeadThreads), 0, s, a, sp.G, sp.rounds, sums ? part : (float*)nullptr);
-        return hipGetLastError();
-      };
-      const hipError_t e = vec ? (norm ? go(heads_grad_kernel<X, Y, true, true>) : go(heads_grad_kernel<X, Y, true, false>))
-                               : (norm ? go(heads_grad_kernel<X, Y, false, true>) : go(heads_grad_kernel<X, Y, false, false>));
+      const HeadsSplit sp = split(a);
+      const int y = chunks(sp);
+      const unsigned blocks = norm ? (unsigned)grad_blocks(a, sp)
+                                   : (unsigned)std::min<int64_t>(token_groups(a, sp), std::max(1, (1 << 18) / y));
+      const dim3 grid(blocks, (unsigned)y);
+      strips[0] = (int)blocks * sp.kind[0].chunks;
+      strips[1] = (int)blocks * sp.kind[1].chunks;
+      int n = std::min(views_elements(a, sizeof(Y)), row_elements(a.dx, a.lddx, a.dh, sizeof(X)));
+      if (norm) n = std::min(n, row_elements(a.x, a.ldx, a.dh, sizeof(X)));
+      auto kernel = n == 8 ? heads_grad_kernel<X, Y, 8> : n == 2 ? heads_grad_kernel<X, Y, 2> : heads_grad_kernel<X, Y, 1>;
+      launch(kernel, grid, dim3(kHeadThreads), 0, s, a, sp, sums ? part : (float*)nullptr);
+      const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    return sums ? launch_cols_join(part, strips, a.dh, dgq, dgk, s) : hipGetLastError();
+    if (sums) launch(heads_gain_kernel, dim3((unsigned)(a.dh + 31) / 32, 2), dim3(1024), 0, s, (const float*)part, strips[0], strips[1], a.dh, dgq, dgk);
+    return hipGetLastError();
   });
 }
 

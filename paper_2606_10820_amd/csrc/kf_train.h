@@ -106,7 +106,7 @@ struct HeadsArgs {
   int64_t lddx;
 };
 hipError_t launch_heads(const HeadsArgs& a, hipStream_t s);
-int heads_strips(const HeadsArgs& a);  // of part [strips][2][dh]
+int heads_strips(const HeadsArgs& a);  // of part [strips][dh]
 hipError_t launch_heads_grad(const HeadsArgs& a, float* dgq, float* dgk, float* part, hipStream_t s);
 hipError_t launch_rope_table(int64_t n, int pairs, double base, float2* table, hipStream_t s);
 

@@ -324,7 +324,7 @@ size_t kf_qkv_heads_backward_bytes(int B, int L, int n_head, int n_kv, int d_hea
   if (heads_args(KF_FP32, KF_FP32, B, L, n_head, n_kv, d_head, nullptr, nullptr, 0.f, nullptr, 0, 0,
                  nullptr, 0, a) != KF_OK)
     return 0;
-  return (size_t)kf::heads_strips(a) * 2 * d_head * sizeof(float);
+  return (size_t)kf::heads_strips(a) * d_head * sizeof(float);
 }
 
 int kf_qkv_heads_backward(void* hip_stream, int x_dtype, int y_dtype, int B, int L, int n_head,
