@@ -503,7 +503,9 @@ def _rows(t, what: str, shape=None):
         raise ValueError(f"{what} must have at least one dimension")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}")
-    d = t.shape[-1]
+    d, n = t.shape[-1], t.numel()
+    if n and t.is_contiguous():
+        return n // d, d
     if t.dim() != 2:
         try:
             t = t.view(-1, d) if t.numel() else t.new_empty((0, d))
@@ -715,24 +717,26 @@ def _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev):
     if table is not None:
         if table.dim() != 3 or table.shape[2] != 2:
             raise ValueError("table must be [n_pos][d_rot / 2][2] (rope_table)")
-        _check(table, "table", dev, torch.float32, table.numel())
         n_pos, d_rot = table.shape[0], 2 * table.shape[1]
+        _check(table, "table", dev, torch.float32, n_pos * d_rot)
     if positions is not None:
-        if positions.shape not in ((L,), (B, L)):
+        n = positions.dim()
+        if n == 2 and positions.shape[0] == B:
+            pos_ld = L
+        elif n != 1:
             raise ValueError("positions must be [L] or [B, L]")
-        _check(positions, "positions", dev, torch.int32, positions.numel())
-        pos_ld = L if positions.dim() == 2 else 0
+        _check(positions, "positions", dev, torch.int32, B * L if n == 2 else L)
     return n_pos, d_rot, pos_ld
 
 
-def _heads_of(t, what, shape, dtype, dev):
+def _heads_of(t, what, B, H, L, dh, dtype, dev):
     """t [B][H][L][dh] (or None) as kf_heads."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype != dtype or t.device != dev:
-        raise ValueError(f"{what} must be {dtype} {tuple(shape)} on {dev}")
+    if t.shape != (B, H, L, dh) or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{what} must be {dtype} {(B, H, L, dh)} on {dev}")
     sb, sh, sl, sc = t.stride()
-    if sc != 1 and shape[3] > 1:
+    if sc != 1 and dh > 1:
         raise ValueError(f"{what}'s last dimension must be contiguous")
     return KfHeads(t.data_ptr(), sb, sh, sl)
 
@@ -761,19 +765,25 @@ def qkv_heads(qkv, n_head: int, n_kv: Optional[int] = None, table=None, position
     with ctx:
         if out is None:
             yt = out_dtype or qkv.dtype
-            out = tuple(torch.empty((B, h, L, dh), dtype=yt, device=dev) for h in (n_head, n_kv, n_kv))
+            q = torch.empty((B, n_head, L, dh), dtype=yt, device=dev)
+            k = torch.empty_like(q) if n_kv == n_head else torch.empty((B, n_kv, L, dh), dtype=yt, device=dev)
+            out = (q, k, torch.empty_like(k))
+            n = L * dh
+            vq = KfHeads(q.data_ptr(), n_head * n, n, dh)
+            vk, vv = (KfHeads(t.data_ptr(), n_kv * n, n, dh) for t in out[1:])
         else:
             if len(out) != 3 or all(t is None for t in out):
                 raise ValueError("out must be (q, k, v), one of them at least a tensor")
+            out = tuple(out)
             yt = next(t.dtype for t in out if t is not None)
             if out_dtype not in (None, yt):
                 raise ValueError("out must be of out_dtype")
-        views = [_heads_of(t, n, (B, h, L, dh), yt, dev)
-                 for t, n, h in zip(out, ("q", "k", "v"), (n_head, n_kv, n_kv))]
+            vq, vk, vv = (_heads_of(t, n, B, h, L, dh, yt, dev)
+                          for t, n, h in zip(out, ("q", "k", "v"), (n_head, n_kv, n_kv)))
         _ok(lib().kf_qkv_heads(s, _type(qkv.dtype, "qkv"), _type(yt, "out"), B, L, n_head, n_kv, dh,
                                qkv.data_ptr(), ldx, _ptr(q_gain), _ptr(k_gain), eps, _ptr(table),
-                               n_pos, d_rot, _ptr(positions), pos_ld, *views))
-    return tuple(out)
+                               n_pos, d_rot, _ptr(positions), pos_ld, vq, vk, vv))
+    return out
 
 
 def qkv_heads_backward(dq, dk, dv, qkv=None, table=None, positions=None, q_gain=None, k_gain=None,
@@ -785,21 +795,23 @@ def qkv_heads_backward(dq, dk, dv, qkv=None, table=None, positions=None, q_gain=
     forward call, needed where there are gains.  dqkv is of qkv's type (without it: out_dtype,
     default dq's); out: where it goes, qkv itself if that is not needed again."""
     import torch
-    for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
-        if t.dim() != 4:
-            raise ValueError(f"{n} must be [B][heads][L][d_head]")
+    if dq.dim() != 4 or dk.dim() != 4:
+        raise ValueError("dq, dk and dv must be [B][heads][L][d_head]")
     B, Hq, L, dh = dq.shape
-    Hkv, dev = dk.shape[1], dq.device
-    shape = (B, L, (Hq + 2 * Hkv) * dh)
-    ldx, xt = shape[2], out_dtype or (out.dtype if out is not None else dq.dtype)
+    Hkv, dev, yt = dk.shape[1], dq.device, dq.dtype
+    ldx = (Hq + 2 * Hkv) * dh
+    shape = (B, L, ldx)
+    xt = out_dtype or (out.dtype if out is not None else yt)
     if qkv is not None:
         _, ldx = _rows(qkv, "qkv", shape)
-        if qkv.device != dev or out_dtype not in (None, qkv.dtype):
-            raise ValueError("qkv must be on dq's device, and dqkv of its type")
         xt = qkv.dtype
+        if qkv.device != dev or out_dtype not in (None, xt):
+            raise ValueError("qkv must be on dq's device, and dqkv of its type")
     elif q_gain is not None or k_gain is not None:
         raise ValueError("gains' gradients need qkv")
     n_pos, d_rot, pos_ld = _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev)
+    vq, vk, vv = (_heads_of(dq, "dq", B, Hq, L, dh, yt, dev), _heads_of(dk, "dk", B, Hkv, L, dh, yt, dev),
+                  _heads_of(dv, "dv", B, Hkv, L, dh, yt, dev))
     s, ctx = _on(dev, stream, (dq, dk, dv, qkv, table, positions, q_gain, k_gain, out))
     with ctx:
         if out is None:
@@ -808,14 +820,15 @@ def qkv_heads_backward(dq, dk, dv, qkv=None, table=None, positions=None, q_gain=
             dx, (_, lddx) = out, _rows(out, "out", shape)
             if dx.device != dev or dx.dtype != xt:
                 raise ValueError("out must be of qkv's type and device")
-        views = [_heads_of(t, n, (B, h, L, dh), dq.dtype, dev)
-                 for t, n, h in ((dq, "dq", Hq), (dk, "dk", Hkv), (dv, "dv", Hkv))]
-        dgq, dgk = (torch.empty(dh, dtype=torch.float32, device=dev) if g is not None else None
-                    for g in (q_gain, k_gain))
-        n = lib().kf_qkv_heads_backward_bytes(B, L, Hq, Hkv, dh) if dgq is not None or dgk is not None else 0
-        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+        dgq = dgk = ws = None
+        n = 0
+        if q_gain is not None or k_gain is not None:
+            dgq, dgk = torch.empty((2, dh), dtype=torch.float32, device=dev).unbind(0)
+            n = lib().kf_qkv_heads_backward_bytes(B, L, Hq, Hkv, dh)
+            ws = torch.empty(n, dtype=torch.uint8, device=dev)
+            dgq, dgk = dgq if q_gain is not None else None, dgk if k_gain is not None else None
         _ok(lib().kf_qkv_heads_backward(
-            s, _type(xt, "qkv"), _type(dq.dtype, "dq"), B, L, Hq, Hkv, dh, *views, _ptr(qkv), ldx,
+            s, _type(xt, "qkv"), _type(yt, "dq"), B, L, Hq, Hkv, dh, vq, vk, vv, _ptr(qkv), ldx,
             _ptr(q_gain), _ptr(k_gain), eps, _ptr(table), n_pos, d_rot, _ptr(positions), pos_ld,
             dx.data_ptr(), lddx, _ptr(dgq), _ptr(dgk), _ptr(ws), n))
     return dx, dgq, dgk
