@@ -60,6 +60,77 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(DropoutArgs a, in
   }
 }
 
+// Rows of any width from 8 on, one after another in memory: eight elements a thread of the
+// whole, in vectors; their numbers are eight halves from half (column % 8) of two groups on,
+// and from the first group of the next row where a row ends among them.
+template <typename X, typename Y, bool RES>
+__global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(DropoutArgs a, int64_t n, int64_t step_row, int step_col) {
+  const DropKey key(a.drop);
+  const int64_t step = (int64_t)gridDim.x * kDropThreads * 8;
+  int64_t at = ((int64_t)blockIdx.x * kDropThreads + threadIdx.x) * 8;
+  int64_t row = at / a.d;
+  int col = (int)(at - row * a.d);
+  for (; at < n; at += step) {
+    const X* x = static_cast<const X*>(a.x) + at;
+    const Y* res = static_cast<const Y*>(a.res) + at;
+    Y* y = static_cast<Y*>(a.y) + at;
+    const int left = (int)min((int64_t)8, n - at);
+    float f[8], r[8];
+    if (left == 8) {
+      load_f<8>(x, f);
+      if constexpr (RES) load_f<8>(res, r);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        f[j] = j < left ? (float)x[j] : 0.f;
+        if constexpr (RES) r[j] = j < left ? (float)res[j] : 0.f;
+      }
+    }
+    if (key.threshold) {
+      // halves from..from + 7 of the 16 of two groups
+      auto halves = [](const uint32_t (&p)[4], const uint32_t (&q)[4], int from, uint32_t (&out)[4]) {
+        const uint32_t w[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+        uint32_t t[6], u[5];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) t[i] = from & 4 ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) u[i] = from & 2 ? t[i + 1] : t[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = from & 1 ? u[i] >> 16 | u[i + 1] << 16 : u[i];
+      };
+      uint32_t p[4], q[4], w[4];
+      const uint32_t group = (uint32_t)col / 8;
+      key.words(p, group, row);
+      key.words(q, group + 1, row);
+      halves(p, q, col & 7, w);
+      const int here = a.d - col;  // elements of this row
+      if (here >= 8) {
+        key.keep<8>(f, w);
+      } else {
+        key.words(p, 0, row + 1);
+        halves(p, p, 8 - here, q);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = key.keep(f[j], j < here ? w[j >> 1] : q[j >> 1], j & 1);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = as_fp32<Y>(RES ? __builtin_fmaf(f[j], key.scale, r[j]) : f[j] * key.scale);
+    if (left == 8) {
+      store_f<8>(y, f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < left) y[j] = (Y)f[j];
+    }
+    row += step_row;
+    col += step_col;
+    if (col >= a.d) {
+      col -= a.d;
+      ++row;
+    }
+  }
+}
+
 }  // namespace
 
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t s) {
@@ -76,6 +147,16 @@ hipError_t launch_dropout(const DropoutArgs& a, hipStream_t s) {
       launch(kernel, dim3(blocks), dim3(kDropThreads), 0, s, a, total, groups, threads / groups, (int)(threads % groups));
       return hipGetLastError();
     };
+    const bool flat = a.d >= 8 && a.ldx == a.d && a.ldy == a.d && (!a.res || a.ldres == a.d) && vector_rows(a.x, 0, 1, 16) &&
+                      vector_rows(a.y, 0, 1, 16) && vector_rows(a.res, 0, 1, 16);
+    if (!vec && flat) {
+      const int64_t n = a.rows * a.d, all = (n + 8 * kDropThreads - 1) / (8 * kDropThreads);
+      const unsigned grid = (unsigned)(all < 4096 ? all : 4096);
+      const int64_t elements = (int64_t)grid * kDropThreads * 8;
+      auto kernel = a.res ? dropout_flat_kernel<X, Y, true> : dropout_flat_kernel<X, Y, false>;
+      launch(kernel, dim3(grid), dim3(kDropThreads), 0, s, a, n, elements / a.d, (int)(elements % a.d));
+      return hipGetLastError();
+    }
     if (vec) return a.res ? go(dropout_kernel<X, Y, true, true>) : go(dropout_kernel<X, Y, true, false>);
     return a.res ? go(dropout_kernel<X, Y, false, true>) : go(dropout_kernel<X, Y, false, false>);
   });

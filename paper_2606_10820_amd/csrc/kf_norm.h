@@ -68,7 +68,8 @@ __device__ __forceinline__ float row_add(float v, float* part) {
 // Dropout of a row held as above: x[v][j] stays, or becomes 0.  Lanes that share groups of
 // eight columns share the generator's calls.  E = 4: the two lanes of a group call it for
 // one vector each of a pair of vectors and swap the halves.  E = 1: eight lanes share a
-// group; each calls it for one vector of eight, and the words go round by lane reads.
+// group; each calls it for one vector of eight and leaves the numbers in LDS, where the
+// wavefront's lanes find theirs.
 template <int LPR, int NV, int E>
 __device__ __forceinline__ void drop_row(const DropKey& key, float (&x)[NV][E], int64_t row, int tid) {
   static_assert(E == 8 || E == 4 || E == 1, "elements a vector");
@@ -102,22 +103,19 @@ __device__ __forceinline__ void drop_row(const DropKey& key, float (&x)[NV][E], 
       key.keep<4>(x[NV - 1], a);
     }
   } else {
+    __shared__ uint4 numbers[kNormThreads];
     const int mine = tid & 7;
 #pragma unroll
     for (int v0 = 0; v0 < NV; v0 += 8) {
       key.words(w, group(v0 + mine), row);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the numbers before have been read
+      numbers[threadIdx.x] = make_uint4(w[0], w[1], w[2], w[3]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      // (of the lane that called it for vector v0 + i: half `mine`)
+      const uint16_t* n = reinterpret_cast<const uint16_t*>(numbers + (threadIdx.x & ~7)) + mine;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (v0 + i >= NV) break;
-        const int from = ((threadIdx.x & 56) + i) * 4;  // the lane that called it for this vector
-        uint32_t word = 0;
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const uint32_t t = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)w[n]);
-          word = mine >> 1 == n ? t : word;
-        }
-        x[v0 + i][0] = key.keep(x[v0 + i][0], word, mine & 1);
-      }
+      for (int i = 0; i < 8 && v0 + i < NV; ++i) x[v0 + i][0] = key.keep(x[v0 + i][0], n[i * 8], 0);
     }
   }
 }

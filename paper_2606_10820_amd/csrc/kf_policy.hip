@@ -18,9 +18,16 @@ namespace {
 // The rows' losses in fp64, in a fixed order.
 __global__ void __launch_bounds__(1024) policy_sum_kernel(const float* __restrict__ row_loss, int64_t rows, float* loss) {
   __shared__ double part[16];
-  double v = 0;
-#pragma unroll 4
-  for (int64_t i = threadIdx.x; i < rows; i += 1024) v += (double)row_loss[i];
+  const int head = (int)min(rows, (int64_t)((-reinterpret_cast<uintptr_t>(row_loss) & 15) / 4));
+  const int64_t n = (rows - head) / 4, tail = head + n * 4;
+  double v = threadIdx.x < head ? row_loss[threadIdx.x] : threadIdx.x < rows - tail ? row_loss[tail + threadIdx.x] : 0.f;
+  if (threadIdx.x < head && threadIdx.x < rows - tail) v += row_loss[tail + threadIdx.x];
+  const float4* p = reinterpret_cast<const float4*>(row_loss + head);
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < n; i += 1024) {
+    const float4 q = p[i];
+    v += ((double)q.x + (double)q.y) + ((double)q.z + (double)q.w);
+  }
   v = block_add<16>(v, part);
   if (threadIdx.x == 0) *loss = (float)v;
 }
