@@ -461,7 +461,7 @@ int kf_token_logprobs_backward(void *hip_stream, int dtype, int64_t rows, int vo
  * d_rot 0 all of them, are not turned.  Value heads are copied.
  *   positions int32: row (b, l) is at positions[b * pos_ld + l] (pos_ld 0: one list of
  *   L for all sequences), or null: at l.  A position outside [0, n_pos) gives NaN in the
- *   turned columns.
+ *   turned columns, and in its row's gradients and the gains'.
  *   q, k, v: where head h of row (b, l) goes, d_head consecutive elements of y_dtype at
  *   ptr + b batch + h head + l row (a view of a larger tensor will do, as a region of
  *   KF_MASK_DOUBLE's keys); heads must not share elements; a null ptr: not wanted.

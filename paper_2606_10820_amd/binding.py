@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import operator
 import os
 from typing import NamedTuple, Optional
 
@@ -504,6 +505,8 @@ def _rows(t, what: str, shape=None):
     if shape is not None and t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}")
     d, n = t.shape[-1], t.numel()
+    if d >> 31:
+        raise ValueError(f"{what}'s rows must be shorter than 2^31 elements")
     if n and t.is_contiguous():
         return n // d, d
     if t.dim() != 2:
@@ -699,7 +702,7 @@ def rope_table(n_pos: int, d_rot: int, base: float = 10000.0, device=None, strea
     dev = torch.device("cuda" if device is None else device)
     if dev.type == "cuda" and dev.index is None:
         dev = torch.device("cuda", torch.cuda.current_device())
-    if n_pos < 1 or d_rot < 2 or d_rot % 2:
+    if n_pos < 1 or n_pos >> 31 or d_rot < 2 or d_rot % 2:
         raise ValueError("a table has positions and an even number of columns")
     s, ctx = _on(dev, stream, ())
     with ctx:
@@ -711,6 +714,8 @@ def rope_table(n_pos: int, d_rot: int, base: float = 10000.0, device=None, strea
 def _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev):
     """(n_pos, d_rot, pos_ld) of qkv_heads' table and positions."""
     import torch
+    if B * L > 1 << 30:
+        raise ValueError("at most 2^30 rows")
     _check(q_gain, "q_gain", dev, torch.float32, dh)
     _check(k_gain, "k_gain", dev, torch.float32, dh)
     n_pos = d_rot = pos_ld = 0
@@ -718,6 +723,8 @@ def _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev):
         if table.dim() != 3 or table.shape[2] != 2:
             raise ValueError("table must be [n_pos][d_rot / 2][2] (rope_table)")
         n_pos, d_rot = table.shape[0], 2 * table.shape[1]
+        if n_pos >> 31:
+            raise ValueError("table must have fewer than 2^31 positions")
         _check(table, "table", dev, torch.float32, n_pos * d_rot)
     if positions is not None:
         n = positions.dim()
@@ -834,11 +841,15 @@ def qkv_heads_backward(dq, dk, dv, qkv=None, table=None, positions=None, q_gain=
     return dx, dgq, dgk
 
 
-def _seed(seed, dev):
+def _seed(seed, site, dev):
     """(host seed, device seed) of an int or of a tensor of one int64 on dev."""
+    if not 0 <= site < 1 << 31:
+        raise ValueError("site must be a number below 2^31")
     if isinstance(seed, int):
         return seed & 0xFFFFFFFFFFFFFFFF, None
     import torch
+    if not isinstance(seed, torch.Tensor):
+        return operator.index(seed) & 0xFFFFFFFFFFFFFFFF, None
     _check(seed, "seed", dev, torch.int64, 1)
     return 0, seed.data_ptr()
 
@@ -862,7 +873,7 @@ def dropout(x, p: float, seed, site: int = 0, residual=None, out_dtype=None, out
         _, ldres = _rows(residual, "residual", x.shape)
         if residual.dtype != yt or residual.device != dev:
             raise ValueError("residual must be of the result's type, on x's device")
-    host, at = _seed(seed, dev)
+    host, at = _seed(seed, site, dev)
     s, ctx = _on(dev, stream, (x, residual, out, None if at is None else seed))
     with ctx:
         if out is None:
@@ -898,7 +909,7 @@ def dropout_norm(x, residual, gain, shift=None, p: float = 0.0, seed=0, site: in
         raise ValueError("residual must be on x's device")
     _check(gain, "gain", dev, torch.float32, d)
     _check(shift, "shift", dev, torch.float32, d)
-    host, at = _seed(seed, dev)
+    host, at = _seed(seed, site, dev)
     s, ctx = _on(dev, stream, (x, residual, gain, shift, out, None if at is None else seed))
     with ctx:
         if out is None:
@@ -934,7 +945,7 @@ def dropout_norm_backward(dy, h, gain, stats, p: float = 0.0, seed=0, site: int 
         raise ValueError("dy must be on h's device")
     _check(gain, "gain", dev, torch.float32, d)
     _check(stats, "stats", dev, torch.float32, 2 * rows)
-    host, at = _seed(seed, dev)
+    host, at = _seed(seed, site, dev)
     s, ctx = _on(dev, stream, (dy, h, gain, stats, dres, None if at is None else seed))
     with ctx:
         dh = torch.empty(h.shape, dtype=h.dtype, device=dev)

@@ -159,6 +159,21 @@ def test_binding_refuses_host_tensors_and_bad_shapes():
             call()
 
 
+def test_binding_refuses_what_32_bits_do_not_hold():
+    """Sizes that the C entries take as 32 bits (tensors without memory)."""
+    big = lambda *s: torch.empty(*s, device="meta", dtype=torch.bfloat16)
+    for call in (lambda: Bd.dropout(big(2 ** 32 + 100), 0.1, 1), lambda: Bd.dropout(big(3, 2 ** 31), 0.1, 1), lambda: Bd.qkv_heads(big(1, 2 ** 32 + 8, 3), 1),
+                 lambda: Bd.qkv_heads(big(2 ** 16, 2 ** 14 + 1, 3), 1), lambda: Bd.qkv_heads_backward(*[big(1, 1, 2 ** 32 + 8, 1)] * 3),
+                 lambda: Bd.qkv_heads(big(1, 8, 6), 1, table=torch.empty(2 ** 32 + 8, 1, 2, device="meta")), lambda: Bd.rope_table(2 ** 32 + 8, 2, device="meta"),
+                 lambda: Bd.policy_loss(big(1, 2 ** 32 + 8), torch.zeros(1, dtype=torch.int32), torch.zeros(1)), lambda: Bd.layer_norm(big(2 ** 32 + 8), big(1)),
+                 lambda: Bd.dropout(big(4, 8), 0.1, 1, site=2 ** 31), lambda: Bd.dropout(big(4, 8), 0.1, 1, site=-1), lambda: Bd.dropout(big(4, 8), 0.1, 1, site=2 ** 32 + 1)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        Bd.dropout(big(4, 8), 0.1, 1.5)
+    assert Bd._seed(np.int64(-1), 0, None) == Bd._seed(-1, 0, None) == (2 ** 64 - 1, None)
+
+
 def test_philox_against_published_vectors():
     n = 0
     for line in open(GOLDEN):
