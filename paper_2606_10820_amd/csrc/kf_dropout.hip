@@ -87,16 +87,19 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(DropoutArgs 
       }
     }
     if (key.threshold) {
+      // (by value: a choice of two array elements is one of addresses, and the arrays go to
+      // scratch memory)
+      auto either = [](bool first, uint32_t a, uint32_t b) { return first ? a : b; };
       // halves from..from + 7 of the 16 of two groups
-      auto halves = [](const uint32_t (&p)[4], const uint32_t (&q)[4], int from, uint32_t (&out)[4]) {
+      auto halves = [&](const uint32_t (&p)[4], const uint32_t (&q)[4], int from, uint32_t (&out)[4]) {
         const uint32_t w[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
         uint32_t t[6], u[5];
 #pragma unroll
-        for (int i = 0; i < 6; ++i) t[i] = from & 4 ? w[i + 2] : w[i];
+        for (int i = 0; i < 6; ++i) t[i] = either(from & 4, w[i + 2], w[i]);
 #pragma unroll
-        for (int i = 0; i < 5; ++i) u[i] = from & 2 ? t[i + 1] : t[i];
+        for (int i = 0; i < 5; ++i) u[i] = either(from & 2, t[i + 1], t[i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = from & 1 ? u[i] >> 16 | u[i + 1] << 16 : u[i];
+        for (int i = 0; i < 4; ++i) out[i] = either(from & 1, u[i] >> 16 | u[i + 1] << 16, u[i]);
       };
       uint32_t p[4], q[4], w[4];
       const uint32_t group = (uint32_t)col / 8;
@@ -110,7 +113,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(DropoutArgs 
         key.words(p, 0, row + 1);
         halves(p, p, 8 - here, q);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = key.keep(f[j], j < here ? w[j >> 1] : q[j >> 1], j & 1);
+        for (int j = 0; j < 8; ++j) f[j] = key.keep(f[j], either(j < here, w[j >> 1], q[j >> 1]), j & 1);
       }
     }
 #pragma unroll

@@ -73,16 +73,18 @@ struct HeadCols {
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float v[2] = {0.f, 0.f};
+        // (lanes past the last column load the first ones: a load behind a branch waits for it)
+        const int at = 2 * pair(i);
+        const bool one = at < dh, two = E == 2 ? one : at + 1 < dh;
+        float v[2];
         if constexpr (E == 2) {
-          if (2 * pair(i) < dh) load_f<2>(p + 2 * pair(i), v);
+          load_f<2>(p + (one ? at : 0), v);
         } else {
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            if (2 * pair(i) + k < dh) v[k] = (float)p[2 * pair(i) + k];
+          v[0] = (float)p[one ? at : 0];
+          v[1] = (float)p[two ? at + 1 : 0];
         }
-        f[2 * i] = v[0];
-        f[2 * i + 1] = v[1];
+        f[2 * i] = one ? v[0] : 0.f;
+        f[2 * i + 1] = two ? v[1] : 0.f;
       }
     }
   }
