@@ -3,8 +3,8 @@
 // half first, for eight columns.  An element is dropped where its number is below
 // `threshold`; the mask depends on nothing else (no stride, no split of the work), so it is
 // formed again wherever it is needed and never stored.  16 bits an element: the generator's
-// ten rounds (20 wide multiplies, a quarter of the rate of others) are paid once in eight
-// elements, which hides them under 4 bytes of memory traffic an element; 32 would not.
+// ten rounds (20 wide multiplies, each at a quarter of an addition's rate) are paid once in
+// eight elements, which hides them under 4 bytes of memory traffic an element.
 #pragma once
 #include <type_traits>
 

@@ -7,7 +7,12 @@
 // or dx = w without gains.  r is formed again from x: that needs no memory of its own, and x
 // is read for dg anyway.  Norms, turns and sums are fp32, each result is rounded once.
 //
-// Bound by memory: each element is read and written once.
+// Bound by memory: each element is read and written once.  40960 rows of 36 heads of 64 bf16
+// with norms, forward 74 us and backward, which reads x again, 99 (5.1 TB/s both); 81920 rows of
+// 48 heads without norms 171 and 190 us (5.9, 5.3).  A few rows are bound by the launch (3.6 us).
+// Heads that are not whole vectors of 16 bytes take pairs or single elements: 40960 x 36 bf16
+// with norms, forward and backward, 105 and 171 us of 80 columns, 160 and 242 of 78, 225 and 293
+// of 77.
 #include <algorithm>
 
 #include "kf_rows.h"
@@ -18,10 +23,13 @@ namespace {
 
 // A head is held by G lanes, a power of two, eight columns each (a pair never leaves its
 // lane): eight in a row where rows are whole vectors of 16 bytes, else four pairs G apart.  A workgroup's heads are of one kind, so that what a kind needs is uniform; a
-// wavefront takes `side` heads (the largest power of two that divides their number, at most
-// 64 / G) of 64 / G / side consecutive tokens at a time, every lane with work, and up to kAhead
-// rounds of further heads of the same tokens with all their loads in flight and their turns
-// loaded once.
+// wavefront takes `side` heads (the largest power of two that divides their number and leaves
+// two tokens) of 64 / G / side consecutive tokens at a time, every lane with work, and up to
+// kAhead rounds of further heads of the same tokens with all their loads in flight and their
+// turns loaded once.  Two tokens: one of them, all lanes on it, writes single rows of each
+// head's plane and reads so in the backward pass (40960 rows, 16 + 8 + 8 heads of 64, forward
+// and backward, 72 and 103 us against 55 and 94; at least four tokens 57 and 118).  kAhead 4:
+// 8 + 8 + 8 heads of 128 forward 86 us, 2 116, 3 119, 6 90.
 constexpr int kHeadThreads = 256, kHeadWaves = kHeadThreads / 64, kAhead = 4;
 
 // The heads of one kind (0 queries, 1 keys, 2 values): `rounds` of them a chunk.
@@ -88,7 +96,8 @@ struct HeadCols {
       }
     }
   }
-  // Past the caches: results are read by other kernels, after all of them are written.
+  // Past the caches: 81920 x 48 heads forward and backward 362 us, through them 401; the
+  // attention that reads the results takes the same time after either.
   template <typename T>
   __device__ __forceinline__ void store(T* p, const float (&f)[8]) const {
     constexpr int P = E == 8 ? 16 / sizeof(T) : E;
@@ -209,9 +218,10 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, HeadsS
 }
 
 // Gains' gradients are summed in registers, a lane's eight columns over its tokens and heads,
-// then over a workgroup's lanes of the same columns, and leave as [dh] of the strip.
+// then over a workgroup's lanes of the same columns, and leave as [dh] of the strip (`direct`:
+// each kind has one strip, whose sums are the result).
 template <typename X, typename Y, int E>
-__global__ void __launch_bounds__(kHeadThreads) heads_grad_kernel(HeadsArgs a, HeadsSplit s, float* part) {
+__global__ void __launch_bounds__(kHeadThreads) heads_grad_kernel(HeadsArgs a, HeadsSplit s, float* part, bool direct, float* dgq, float* dgk) {
   __shared__ float sums[kHeadWaves][512];
   const HeadsAt at(a, s);
   const HeadCols<E> cols{(int)(threadIdx.x & ((1 << s.G_log) - 1)), 1 << s.G_log, a.dh};
@@ -279,6 +289,10 @@ __global__ void __launch_bounds__(kHeadThreads) heads_grad_kernel(HeadsArgs a, H
   }
   __syncthreads();
   float* to = part + (size_t)(blockIdx.y * gridDim.x + blockIdx.x) * a.dh;
+  if (direct) {
+    to = at.kind ? dgk : dgq;
+    if (!to) return;
+  }
   for (int i = threadIdx.x; i < a.dh; i += kHeadThreads) {
     float v = sums[0][i];
 #pragma unroll
@@ -381,7 +395,8 @@ hipError_t launch_heads(const HeadsArgs& a, hipStream_t s) {
   });
 }
 
-// Workgroups with sums, at most, over all chunks.
+// Workgroups with sums, at most, over all chunks (40960 rows, 16 + 8 + 8 heads of 64, backward:
+// 1024 115 us, 2048 and 4096 95, 16384 113).
 constexpr int kHeadStrips = 2048;
 namespace {
 int grad_blocks(const HeadsArgs& a, const HeadsSplit& sp) {
@@ -399,6 +414,7 @@ hipError_t launch_heads_grad(const HeadsArgs& a, float* dgq, float* dgk, float* 
     using Y = decltype(yt);
     const bool norm = a.gq || a.gk, sums = dgq || dgk;
     int strips[2] = {0, 0};
+    bool joined = false;
     if (a.B && a.L) {
       const HeadsSplit sp = split(a);
       const int y = chunks(sp);
@@ -410,11 +426,13 @@ hipError_t launch_heads_grad(const HeadsArgs& a, float* dgq, float* dgk, float* 
       int n = std::min(views_elements(a, sizeof(Y)), row_elements(a.dx, a.lddx, a.dh, sizeof(X)));
       if (norm) n = std::min(n, row_elements(a.x, a.ldx, a.dh, sizeof(X)));
       auto kernel = n == 8 ? heads_grad_kernel<X, Y, 8> : n == 2 ? heads_grad_kernel<X, Y, 2> : heads_grad_kernel<X, Y, 1>;
-      launch(kernel, grid, dim3(kHeadThreads), 0, s, a, sp, sums ? part : (float*)nullptr);
+      // (a gain without heads of its kind has no strip: the join writes zeros)
+      joined = (!dgq || strips[0] == 1) && (!dgk || strips[1] == 1);
+      launch(kernel, grid, dim3(kHeadThreads), 0, s, a, sp, sums ? part : (float*)nullptr, joined, dgq, dgk);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    if (sums) launch(heads_gain_kernel, dim3((unsigned)(a.dh + 31) / 32, 2), dim3(1024), 0, s, (const float*)part, strips[0], strips[1], a.dh, dgq, dgk);
+    if (sums && !joined) launch(heads_gain_kernel, dim3((unsigned)(a.dh + 31) / 32, 2), dim3(1024), 0, s, (const float*)part, strips[0], strips[1], a.dh, dgq, dgk);
     return hipGetLastError();
   });
 }

@@ -185,6 +185,7 @@ __device__ __forceinline__ void policy_row(int64_t row, int tok, float lp, float
   if (a.ratio) a.ratio[row] = ratio;
   if (a.kl) a.kl[row] = kl;
   a.row_loss[row] = loss;
+  if (a.rows == 1 && a.loss) *a.loss = loss;
 }
 
 // Alternatives' candidates kept in LDS.  The n-th of 64 sets' maxima is passed by about

@@ -291,6 +291,20 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(A a) {
     }
     if (sub) return;
   }
+  if constexpr (kDrop) {
+    if (gridDim.x == 1) {  // the only strip's sums are the result
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (c.on[v]) {
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            if (a.dgain) a.dgain[c.col[v] + j] = ag[v][j];
+            if (a.dshift) a.dshift[c.col[v] + j] = ab[v][j];
+          }
+        }
+      return;
+    }
+  }
   float* p = a.part + (size_t)blockIdx.x * 2 * a.d;
 #pragma unroll
   for (int v = 0; v < NV; ++v)

@@ -228,3 +228,16 @@ def test_rope_table(Bd, n, rot, base):
     assert t.shape == (n, rot // 2, 2)
     for got, want in ((t[..., 0], torch.cos(a)), (t[..., 1], torch.sin(a))):
         assert bool(((got - want).abs() <= R.U * want.abs() + 1e-10).all())
+
+
+@pytest.mark.parametrize("L", [1, 2, 5, 40])
+@pytest.mark.parametrize("Hq,Hkv", [(2, 0), (0, 2), (1, 1), (12, 3)])
+def test_few_rows_and_single_gains(Bd, L, Hq, Hkv):
+    """One workgroup's sums are written without a second launch, several are joined; a gain that has no
+    heads has gradient 0; either gradient alone."""
+    for dh in (64, 7):
+        for norm in ((True, True), (True, False), (False, True)):
+            x, table, gains, grads = _inputs(1, L, Hq, Hkv, dh, 4, BF, BF, norm=norm)
+            _, _, dgq, dgk = _both(Bd, x, Hq, Hkv, dh, table, None, gains, grads, BF, str(norm))
+            assert dgq is None or Hq or not dgq.any()
+            assert dgk is None or Hkv or not dgk.any()

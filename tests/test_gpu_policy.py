@@ -207,3 +207,17 @@ def test_repeats_are_equal(Bd):
     a = run()
     for _ in range(3):
         assert all(torch.equal(s, t) for s, t in zip(a, run()))
+
+
+def test_not_a_number_stays_in_its_row(Bd):
+    """NaN or plus infinity among a row's logits, or NaN in what the loss is formed from, makes that row's
+    loss and gradient NaN and no other's."""
+    for V in (90, 3000, 40000):
+        x, _, adv, old, ref, _ = _inputs(8, V, F32)
+        tok = torch.arange(8, dtype=torch.int32)
+        x[0, 50], x[1, 20], adv[2], old[3], ref[4] = NAN, INF, NAN, NAN, NAN
+        r = Bd.policy_loss(x.cuda(), tok.cuda(), adv.cuda(), old.cuda(), ref.cuda(), kl_coef=0.1, entropy_coef=0.01)
+        bad = torch.arange(8) < 5
+        assert torch.equal(torch.isnan(r.row_loss).cpu(), bad) and torch.isnan(r.loss)
+        assert torch.equal(torch.isnan(r.d_logits).all(-1).cpu(), bad) and torch.isfinite(r.d_logits.cpu()[~bad]).all()
+        assert torch.isfinite(r.logp.cpu()[2:]).all() and torch.isfinite(r.entropy.cpu()[2:]).all()
