@@ -22,11 +22,12 @@ namespace kf {
 namespace {
 
 // A head is held by G lanes, a power of two, eight columns each (a pair never leaves its
-// lane): eight in a row where rows are whole vectors of 16 bytes, else four pairs G apart.  A workgroup's heads are of one kind, so that what a kind needs is uniform; a
-// wavefront takes `side` heads (the largest power of two that divides their number and leaves
-// two tokens) of 64 / G / side consecutive tokens at a time, every lane with work, and up to
-// kAhead rounds of further heads of the same tokens with all their loads in flight and their
-// turns loaded once.  Two tokens: one of them, all lanes on it, writes single rows of each
+// lane): eight in a row where rows are whole vectors of 16 bytes, else four pairs G apart.
+// A workgroup's heads are of one kind, so that what a kind needs is uniform; a wavefront
+// takes `side` heads (the largest power of two that divides their number and leaves two
+// tokens) of 64 / G / side consecutive tokens at a time, every lane with work, and up to kAhead
+// rounds of further heads of the same tokens with all their loads in flight and their turns
+// loaded once.  Two tokens: one of them, all lanes on it, writes single rows of each
 // head's plane and reads so in the backward pass (40960 rows, 16 + 8 + 8 heads of 64, forward
 // and backward, 72 and 103 us against 55 and 94; at least four tokens 57 and 118).  kAhead 4:
 // 8 + 8 + 8 heads of 128 forward 86 us, 2 116, 3 119, 6 90.

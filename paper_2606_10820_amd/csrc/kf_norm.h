@@ -120,6 +120,11 @@ __device__ __forceinline__ void drop_row(const DropKey& key, float (&x)[NV][E], 
   }
 }
 
+__device__ __forceinline__ DropKey drop_key(const DropNormArgs& a) { return DropKey(a.drop); }
+__device__ __forceinline__ DropKey drop_key(const DropNormGradArgs& a) { return DropKey(a.drop); }
+__device__ __forceinline__ int drop_key(const NormArgs&) { return 0; }
+__device__ __forceinline__ int drop_key(const NormGradArgs&) { return 0; }
+
 // The gain and shift stay in registers over the workgroup's rows.  With A = DropNormArgs the
 // rows are formed first, h = res + dropout(in), and stored; their norm is of what is stored.
 template <typename X, typename Y, int E, int EPL, int LPR, typename A>
@@ -134,6 +139,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(A a) {
   float g[NV][E], b[NV][E];
   c.load(g, a.gain);
   if (a.shift) c.load(b, a.shift);
+  [[maybe_unused]] const auto key = drop_key(a);
   int turn = 0;
   for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
     const int64_t row = row0 + threadIdx.x / LPR;
@@ -144,7 +150,6 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(A a) {
       float in[NV][E];
       c.stream(in, static_cast<const Y*>(a.in) + at * a.ldin);
       c.load(x, static_cast<const X*>(a.res) + at * a.ldres);
-      const DropKey key(a.drop);
       drop_row<LPR>(key, in, at, tid);
       X* h = static_cast<X*>(a.h) + at * a.ldh;
 #pragma unroll
@@ -215,6 +220,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(A a) {
   for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int j = 0; j < E; ++j) ag[v][j] = ab[v][j] = 0.f;
+  [[maybe_unused]] const auto key = drop_key(a);
   int turn = 0;
   for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
     const int64_t row = row0 + sub;
@@ -253,7 +259,6 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(A a) {
       if (c.on[v]) store_f<E>(dx + c.col[v], x[v]);
     }
     if constexpr (kDrop) {
-      const DropKey key(a.drop);
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
