@@ -8,7 +8,7 @@
 //
 // Bound by memory: res, in, h and y once; h, dy, dres, dh and din once.  40960 x 768, fp32
 // stream and bf16 product, 65 us forward (5.8 TB/s) and 82 backward (6.1), one operator after
-// the other 96 and 98; 81920 x 1024 bf16 119 and 157 (5.7, 5.3).  Widths off whole vectors
+// the other 96 and 102; 81920 x 1024 bf16 121 and 157 (5.5, 5.3).  Widths off whole vectors
 // take single elements (40960 x 771: 88 and 111 us against 69 and 95 of 768, measured by whole
 // calls).  bf16 rows of 513 to 768 columns use 75 % of their lanes: the gradient at 40960 x 768
 // takes 70 us where vectors of four in 64 lanes took 62, with another order of a row's sums than

@@ -4,9 +4,9 @@
 //
 // Bound by memory: a thread takes eight columns of a row at a time, one call of the
 // generator, and forms the mask where it needs it.  40960 x 768 bf16 into an fp32 residual
-// 56 us (5.7 TB/s), the gradient 30; of 771 columns 57 and 35.  Rows apart that are not whole
-// vectors go element by element (771 columns so: 197 us).  A few rows are bound by the launch
-// (2.4 us).
+// 56 us (5.7 TB/s), the gradient 36; again and again on the same rows, which the caches hold
+// in part, 56 and 30, and of 771 columns 57 and 35.  Rows apart that are not whole vectors go
+// element by element (771 columns so: 197 us).  A few rows are bound by the launch (2.4 us).
 #include "kf_dropout.h"
 #include "kf_train.h"
 

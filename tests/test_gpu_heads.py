@@ -241,3 +241,34 @@ def test_few_rows_and_single_gains(Bd, L, Hq, Hkv):
             _, _, dgq, dgk = _both(Bd, x, Hq, Hkv, dh, table, None, gains, grads, BF, str(norm))
             assert dgq is None or Hq or not dgq.any()
             assert dgk is None or Hkv or not dgk.any()
+
+
+def test_double_mask_layout(Bd):
+    """The DoubleForward mask's keys, [context | Future-1 | Future-2], from two products straight into the
+    regions of one tensor, and their gradients back out of it."""
+    B, N, K, H, dh = 2, 5, 3, 2, 32
+    rows = 2 * N * K
+    g = torch.Generator().manual_seed(0)
+    ctx, fut = (torch.randn(B, n, 3 * H * dh, generator=g).to(BF).cuda() for n in (N, rows))
+    t = torch.arange(N)[:, None] + 1 + torch.arange(K)
+    pos = torch.cat([t.reshape(-1), (t + K).reshape(-1)]).int().cuda()
+    table = Bd.rope_table(N + 2 * K, dh)
+    gain = torch.full((dh,), 1.1, device="cuda")
+    k, v = (torch.empty(B, H, N + rows, dh, dtype=BF, device="cuda") for _ in range(2))
+    q = torch.empty(B, H, rows, dh, dtype=BF, device="cuda")
+    args = (table, None, gain, gain)
+    Bd.qkv_heads(ctx, H, None, *args, out=(None, k[:, :, :N], v[:, :, :N]))
+    Bd.qkv_heads(fut, H, None, table, pos, gain, gain, out=(q, k[:, :, N:], v[:, :, N:]))
+    a, b = Bd.qkv_heads(ctx, H, None, *args), Bd.qkv_heads(fut, H, None, table, pos, gain, gain)
+    assert torch.equal(q, b[0]) and torch.equal(k, torch.cat([a[1], b[1]], 2)) and torch.equal(v, torch.cat([a[2], b[2]], 2))
+    o, lse = Bd.training_attention_lse(Bd.KF_MASK_DOUBLE, q, k, v, N, K)
+    dq, dk, dv = Bd.training_attention_backward(Bd.KF_MASK_DOUBLE, q, k, v, o, lse, o, N, K)
+    got = Bd.qkv_heads_backward(dq, dk[:, :, N:], dv[:, :, N:], fut, table, pos, gain, gain)
+    want = Bd.qkv_heads_backward(dq, dk[:, :, N:].contiguous(), dv[:, :, N:].contiguous(), fut, table, pos, gain, gain)
+    assert all(torch.equal(s, t) for s, t in zip(got, want))
+    zero = torch.zeros(B, H, 1, 1, dtype=BF, device="cuda").expand(B, H, N, dh)
+    with pytest.raises(ValueError):  # a head's columns are consecutive
+        Bd.qkv_heads_backward(zero, dk[:, :, :N], dv[:, :, :N], ctx, *args)
+    zero = torch.zeros(1, 1, 1, dh, dtype=BF, device="cuda").expand(B, H, N, dh)
+    d, _, dgk = Bd.qkv_heads_backward(zero, dk[:, :, :N], dv[:, :, :N], ctx, *args)
+    assert not d[..., :H * dh].any() and d[..., H * dh:].any() and dgk.any()
