@@ -230,6 +230,9 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
   constexpr int NL = NT < 64 ? NT : 64;  // lanes of one wavefront that share a row
   constexpr bool kPolicy = std::is_same<A, PolicyArgs>::value;
   constexpr bool kTop = !GRAD && !kPolicy && NT >= 64;
+  // A gradient's row that registers do not hold is read again soon: through the caches (2000 x
+  // 131072 fp32 542 -> 495 us, 2000 x 151936 bf16 333 -> 280; last part first, 1 to 3 % more, not kept).
+  constexpr bool kTwice = GRAD && NV == 0;
   __shared__ RowShared<NT> shared[kTop || NW > 1 ? RPB : 1];
   RowShared<NT>& sh = shared[kTop || NW > 1 ? threadIdx.x / NT : 0];
   const int tid = threadIdx.x % NT, lane = tid & 63, V = a.vocab;
@@ -256,7 +259,8 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
 #pragma unroll
       for (int j = 0; j < NR; ++j) {
         r[j] = u32x4{R::kFill, R::kFill, R::kFill, R::kFill};
-        if (first + j * NT + tid < have) r[j] = __builtin_nontemporal_load(xv + first + j * NT + tid);
+        if (first + j * NT + tid < have)
+          r[j] = kTwice ? xv[first + j * NT + tid] : __builtin_nontemporal_load(xv + first + j * NT + tid);
       }
     };
     // f(vector, its index) over this thread's vectors; past the row's last one a

@@ -212,3 +212,21 @@ def test_norm_strides_and_in_place(Bd, pair, off, ld):
     assert all(torch.equal(a, b) for a, b in zip((dh, dx, dg, db), want))
     Rs.fill_(7.0)
     assert (rbuf == 7).all()
+
+
+def test_norm_past_32_bits(Bd):
+    """Rows past 2^31 elements, both ways."""
+    rows, d = 270_000, 8192
+    x = torch.empty(rows, d, dtype=BF, device="cuda")
+    x.normal_()
+    gain = torch.ones(d, device="cuda")
+    h, y, st = Bd.dropout_norm(x, x, gain, None, 0.25, 21, 2)
+    ref, b = S.dropout(x[-3:].cpu(), 0.25, 21, 2, x[-3:].cpu(), BF, rows - 3)
+    assert R.worst(h[-3:], ref, b) <= 1
+    last = h[-3:].cpu()
+    assert R.worst(y[-3:], R.norm(last, gain.cpu(), None, 1e-5, False)[0], R.norm_bound(last, gain.cpu(), None, 1e-5, False, BF)) <= 1
+    dh, dx, _, _ = Bd.dropout_norm_backward(y, h, gain, st, 0.25, 21, 2)
+    (rdh, _, _), (bdh, _, _) = R.norm_grad(y[-3:].cpu(), last, gain.cpu(), 1e-5, False)
+    assert R.worst(dh[-3:], rdh, bdh) <= 1
+    ref, b = S.dropout(dh[-3:].cpu(), 0.25, 21, 2, None, BF, rows - 3)
+    assert R.worst(dx[-3:], ref, b + 1e-300) <= 1

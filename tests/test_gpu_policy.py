@@ -221,3 +221,19 @@ def test_not_a_number_stays_in_its_row(Bd):
         assert torch.equal(torch.isnan(r.row_loss).cpu(), bad) and torch.isnan(r.loss)
         assert torch.equal(torch.isnan(r.d_logits).all(-1).cpu(), bad) and torch.isfinite(r.d_logits.cpu()[~bad]).all()
         assert torch.isfinite(r.logp.cpu()[2:]).all() and torch.isfinite(r.entropy.cpu()[2:]).all()
+
+
+def test_past_32_bits(Bd):
+    """Offsets past 2^31 elements: the last rows of 2.2e9 logits."""
+    rows, V = 270_000, 8192
+    assert rows * V > 2 ** 31
+    x = torch.empty(rows, V, dtype=BF, device="cuda")
+    x.normal_()
+    tok = torch.full((rows,), 7, dtype=torch.int32, device="cuda")
+    adv, w = torch.ones(rows, device="cuda"), torch.full((rows,), 1.0 / rows, device="cuda")
+    r = Bd.policy_loss(x, tok, adv, weights=w, entropy_coef=0.1)
+    c = float(torch.tensor(0.1))
+    want = S.policy(x[-3:].cpu(), tok[-3:].cpu(), adv[-3:].cpu(), None, None, w[-3:].cpu(), 0.8, 1.2, 0.0, c)
+    for n in ("logp", "entropy", "row_loss", "d_logits"):
+        assert R.worst(getattr(r, n)[-3:], want[n], want[n + "_b"]) <= 1, n
+    assert abs(float(r.loss) - float(r.row_loss.double().sum())) <= R.U * abs(float(r.loss)) + 1e-12
