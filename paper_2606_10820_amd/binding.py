@@ -988,8 +988,8 @@ def policy_loss(logits, tokens, advantages, old_logp=None, ref_logp=None, weight
     advantages, old_logp (None: on policy), ref_logp (None: no KL term), weights (None: ones)
     [...] fp32.  The ratio is clipped to [1 - clip_low, 1 + clip_high].  loss, 0-dimensional, is
     the sum of row_loss, which has the weights in it: give weights of 1 / tokens for a mean.  A
-    row with a negative token or of weight 0 counts nothing: its results are 0.  out: where d_logits goes, logits itself if
-    they are not needed again.  No autograd graph."""
+    row with a negative token or of weight 0 counts nothing: its results are 0.  out: where
+    d_logits goes, logits itself if they are not needed again.  No autograd graph."""
     import torch
     rows, ld = _rows(logits, "logits")
     lead, V, dev = logits.shape[:-1], logits.shape[-1], logits.device
