@@ -351,6 +351,12 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
       rebase(mw, m);
       s = wave_add(s);
       w = wave_add(w);
+      // (a product before a sum may be joined with it on one side of a pair of lanes: their sums then
+      // differ in the last bit, and u, from a small difference of logp, in more)
+      if constexpr (kPolicy) {
+        s = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s)));
+        w = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(w)));
+      }
     }
     const bool empty = s == 0.f;
     const float ls = logf(s), H = empty ? 0.f : ls - kLn2 * w / s;
