@@ -122,9 +122,10 @@ struct Raw<f16> {
   }
 };
 
-// e^d - d - 1 without cancellation: the series to d^9 up to |d| = 1/2 (the next term is 1e-9
-// of the sum), exp2 beyond.
-__device__ __forceinline__ float exp_beyond_linear(float d) {
+// kl = e^d - d - 1 without cancellation, and its derivative e^d - 1: the series to d^9 up to
+// |d| = 1/2 (the next term is 1e-9 of the sum), exp2 beyond.  (Not kl + d there: kl has lost the 1
+// where d is below -2^24, and some of its bits before.)
+__device__ __forceinline__ void exp_beyond_linear(float d, float& kl, float& slope) {
   float p = 1.0f / 362880;
   p = __builtin_fmaf(p, d, 1.0f / 40320);
   p = __builtin_fmaf(p, d, 1.0f / 5040);
@@ -133,8 +134,12 @@ __device__ __forceinline__ float exp_beyond_linear(float d) {
   p = __builtin_fmaf(p, d, 1.0f / 24);
   p = __builtin_fmaf(p, d, 1.0f / 6);
   p = __builtin_fmaf(p, d, 0.5f) * d * d;
-  const float e = __builtin_amdgcn_exp2f(d * kLog2e);
-  return fabsf(d) < 0.5f ? p : d == INFINITY ? INFINITY : (e - 1.0f) - d;
+  slope = __builtin_amdgcn_exp2f(d * kLog2e) - 1.0f;
+  kl = d == INFINITY ? INFINITY : slope - d;
+  if (fabsf(d) < 0.5f) {
+    kl = p;
+    slope = p + d;
+  }
 }
 
 // The kernel's arguments (its only one is a PolicyArgs), read where they are used: kept from
@@ -167,11 +172,11 @@ __device__ __forceinline__ void policy_row(int64_t row, int tok, float lp, float
     loss = cut ? -clipped : -plain;
     u = cut ? 0.f : -plain;
     if (a.ref_logp) {
-      const float d = a.ref_logp[row] - lp;
-      kl = exp_beyond_linear(d);
+      float slope;
+      exp_beyond_linear(a.ref_logp[row] - lp, kl, slope);
       if (a.kl_coef != 0.f) {
         loss += a.kl_coef * kl;
-        u -= a.kl_coef * (d == -INFINITY ? -1.f : kl + d);  // e^d - 1
+        u -= a.kl_coef * slope;
       }
     }
     if (a.entropy_coef != 0.f) loss -= a.entropy_coef * H;
