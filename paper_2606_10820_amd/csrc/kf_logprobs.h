@@ -164,7 +164,7 @@ __device__ __forceinline__ void policy_row(int64_t row, int tok, float lp, float
   float loss = 0.f, ratio = 0.f, kl = 0.f;
   if (tok >= 0) {
     const float A = a.advantage[row], w = a.weight ? a.weight[row] : 1.f;
-    ratio = a.old_logp ? __builtin_amdgcn_exp2f((lp - a.old_logp[row]) * kLog2e) : 1.f;
+    ratio = a.old_logp ? __builtin_amdgcn_exp2f((lp - a.old_logp[row]) * kLog2e) : lp != lp ? lp : 1.f;
     // (a ratio past fp32 meets an advantage of 0 as a number; NaN stays NaN in what follows)
     const float plain = (ratio > 3.4028235e38f ? 3.4028235e38f : ratio) * A;
     const float clipped = (ratio < a.clip_low ? a.clip_low : ratio > a.clip_high ? a.clip_high : ratio) * A;
