@@ -552,6 +552,7 @@ int kf_dropout_norm_backward(void *hip_stream, int norm, int h_dtype, int y_dtyp
  * with A = advantage[row], and loss, one number, the sum of row_loss (formed in fp64).  The
  * gradient with u = -ratio A where ratio A is the lesser (or equal), else 0, less kl_coef (e^g - 1):
  *     d_logits[v] = weight (u ([v = t] - p_v) + entropy_coef p_v (log p_v + entropy))
+ * A ratio past fp32 counts there as fp32's largest number (as a result it is infinity).
  * tokens int32 [rows].  A row whose token is negative or whose weight is 0 counts nothing: every
  * result of it is 0, whatever its logits hold; they are not read.  A token >= vocab gives NaN.
  * A token of logit minus infinity has logp minus infinity, ratio 0 (on policy 1) and, with a

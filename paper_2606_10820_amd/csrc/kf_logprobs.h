@@ -165,9 +165,9 @@ __device__ __forceinline__ void policy_row(int64_t row, int tok, float lp, float
   if (tok >= 0) {
     const float A = a.advantage[row], w = a.weight ? a.weight[row] : 1.f;
     ratio = a.old_logp ? __builtin_amdgcn_exp2f((lp - a.old_logp[row]) * kLog2e) : lp != lp ? lp : 1.f;
-    // (a ratio past fp32 meets an advantage of 0 as a number; NaN stays NaN in what follows)
-    const float plain = (ratio > 3.4028235e38f ? 3.4028235e38f : ratio) * A;
-    const float clipped = (ratio < a.clip_low ? a.clip_low : ratio > a.clip_high ? a.clip_high : ratio) * A;
+    // (a ratio past fp32 counts as the largest number, on both sides of the comparison; NaN stays NaN)
+    const float rho = ratio > 3.4028235e38f ? 3.4028235e38f : ratio, plain = rho * A;
+    const float clipped = (rho < a.clip_low ? a.clip_low : rho > a.clip_high ? a.clip_high : rho) * A;
     const bool cut = plain > clipped;
     loss = cut ? -clipped : -plain;
     u = cut ? 0.f : -plain;
