@@ -557,7 +557,8 @@ int kf_dropout_norm_backward(void *hip_stream, int norm, int h_dtype, int y_dtyp
  * result of it is 0, whatever its logits hold; they are not read.  A token >= vocab gives NaN.
  * A token of logit minus infinity has logp minus infinity, ratio 0 (on policy 1) and, with a
  * reference, kl plus infinity (with a kl_coef its row's loss and gradient are not finite).  NaN or
- * plus infinity in a row's logits makes its loss and gradient NaN, on policy too.  advantage, old_logp,
+ * plus infinity in a row's logits makes its loss and gradient NaN, on policy too.  A row of nothing
+ * but minus infinity has gradient 0 where its loss is finite, else NaN.  advantage, old_logp,
  * ref_logp, weight: fp32 [rows].
  *   row_loss fp32 [rows] is written always; logp, ratio, kl (needs ref_logp), entropy fp32
  *   [rows] and loss fp32 [1] each may be null.

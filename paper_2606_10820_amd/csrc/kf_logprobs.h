@@ -381,8 +381,10 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) __attribute__((amdgpu_wav
         if (tok >= V) u = NAN;
         c = a.d_entropy ? a.d_entropy[row] : 0.f;
       }
-      const float inv = empty ? 0.f : 1.0f / s, at = empty ? 0.f : u;
-      const float k0 = empty ? 0.f : -(u + c * (H - ls)) * inv, k1 = -c * kLn2 * inv;
+      // (a policy row of nothing but minus infinity: 0 where its loss is finite, else NaN)
+      const float none = kPolicy ? u - u : 0.f;
+      const float inv = empty ? 0.f : 1.0f / s, at = empty ? none : u;
+      const float k0 = empty ? none : -(u + c * (H - ls)) * inv, k1 = -c * kLn2 * inv;
       auto grad = [&](float v) {
         const float t = (v - mr) * kLog2e, e = __builtin_amdgcn_exp2f(t);
         return e * __builtin_fmaf(k1, fmaxf(t, kNoShare), k0);
