@@ -562,8 +562,8 @@ int kf_dropout_norm_backward(void *hip_stream, int norm, int h_dtype, int y_dtyp
  * ref_logp, weight: fp32 [rows].
  *   row_loss fp32 [rows] is written always; logp, ratio, kl (needs ref_logp), entropy fp32
  *   [rows] and loss fp32 [1] each may be null.
- *   d_logits (null: no gradient) of dtype, ldd apart; it may be logits (ldd = ld), otherwise
- *   they must not overlap.
+ *   d_logits (null: no gradient) of dtype, ldd apart; it may be logits (ldd = ld).  Otherwise
+ *   results must not overlap the arguments or each other.
  * 0 <= clip_low <= 1 <= clip_high (infinity: not clipped), kl_coef and entropy_coef finite and
  * at most 1e18 in size, 1 <= vocab <= 2^28, 0 <= rows (0: loss becomes 0). */
 int kf_policy_loss(void *hip_stream, int dtype, int64_t rows, int vocab, const void *logits,

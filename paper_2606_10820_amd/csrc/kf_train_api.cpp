@@ -449,6 +449,16 @@ int kf_policy_loss(void* hip_stream, int dtype, int64_t rows, int vocab, const v
         !aligned_or_null(logp, 4) || !aligned_or_null(ratio, 4) || !aligned_or_null(kl, 4) || !aligned_or_null(entropy, 4) ||
         (d_logits && !aligned(d_logits, type_bytes(dtype))) || (d_logits == logits && ld != ldd))
       return KF_EINVAL;
+    // (a row's threads read its arguments while one of them writes its results)
+    const void* const results[] = {d_logits, row_loss, logp, ratio, kl, entropy, loss};
+    const void* const arguments[] = {logits, tokens, advantage, old_logp, ref_logp, weight};
+    for (int i = 0; i < 7; ++i) {
+      if (!results[i]) continue;
+      for (int j = 0; j < i; ++j)
+        if (results[j] == results[i]) return KF_EINVAL;
+      for (int j = i ? 0 : 1; j < 6; ++j)
+        if (arguments[j] == results[i]) return KF_EINVAL;
+    }
   }
   kf::PolicyArgs a = {};
   a.dtype = dtype, a.rows = rows, a.vocab = vocab, a.logits = logits, a.ld = ld, a.tokens = tokens;
