@@ -764,7 +764,7 @@ def qkv_heads(qkv, n_head: int, n_kv: Optional[int] = None, table=None, position
     q_gain, k_gain [d_head] fp32: an RMS norm of each query and key head.  table (rope_table),
     positions [L] or [B, L] int32 (default 0..L-1): rotary positions of queries and keys.
     out: (q, k, v) to write, each a tensor or view of that shape, or None for one that is not
-    wanted.  n_kv defaults to n_head.  No autograd graph."""
+    wanted; or one tensor of the three.  n_kv defaults to n_head.  No autograd graph."""
     import torch
     if qkv.dim() != 3:
         raise ValueError("qkv must be [B, L, (n_head + 2 n_kv) d_head]")
@@ -776,7 +776,7 @@ def qkv_heads(qkv, n_head: int, n_kv: Optional[int] = None, table=None, position
     dh, dev = W // H, qkv.device
     _, ldx = _rows(qkv, "qkv")
     n_pos, d_rot, pos_ld = _heads_args(B, L, dh, table, positions, q_gain, k_gain, dev)
-    s, ctx = _on(dev, stream, (qkv, table, positions, q_gain, k_gain, *(out or ())))
+    s, ctx = _on(dev, stream, (qkv, table, positions, q_gain, k_gain, *(() if out is None else out)))
     with ctx:
         if out is None:
             yt = out_dtype or qkv.dtype
