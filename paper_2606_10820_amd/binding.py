@@ -807,8 +807,9 @@ def qkv_heads_backward(dq, dk, dv, qkv=None, table=None, positions=None, q_gain=
     dq_gain, dk_gain), the last two fp32 [d_head], or None without that gain.
 
     dq [B][n_head][L][d_head], dk and dv [B][n_kv][L][d_head], a head's columns consecutive, of any
-    strides otherwise (gradients expanded over columns too are refused); qkv as in the forward call, needed where there are gains.  dqkv is of qkv's type (without it: out_dtype,
-    default dq's); out: where it goes, qkv itself if that is not needed again."""
+    strides otherwise (gradients expanded over columns too are refused); qkv as in the forward
+    call, needed where there are gains.  dqkv is of qkv's type (without it: out_dtype, default
+    dq's); out: where it goes, qkv itself if that is not needed again."""
     import torch
     if dq.dim() != 4 or dk.dim() != 4:
         raise ValueError("dq, dk and dv must be [B][heads][L][d_head]")

@@ -1,5 +1,6 @@
 // kf_rows.h -- element types, vector loads and reductions of the operators over
-// rows and flat tensors (norms, token log probabilities, gradient clipping).
+// rows and flat tensors (norms, token log probabilities and the policy loss, a QKV
+// product's heads, dropout with and without a norm, gradient clipping).
 #pragma once
 #include <math.h>
 
@@ -78,7 +79,9 @@ __device__ __forceinline__ void stream_out(T* __restrict__ p, const float (&v)[E
 }
 
 // Reductions over a wavefront without LDS: rotations within 16 lanes, then two
-// lane swaps; every lane ends with the result, of the same order in every lane.
+// lane swaps; every lane ends with the result, of the same order in every lane (a
+// product that is summed may be joined with the first sum on one side of each pair
+// of lanes: then they differ in the last bit).
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
